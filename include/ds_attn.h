@@ -317,6 +317,72 @@ ds_status_t ds_attend_rows(const void *q, const void *KV_rows, float *out,
                            const ds_shape_t *shape, void *stream);
 
 /*
+ * Attention over whole prompts, and parts of prompts (Sec. 2.1, causal): what produces the outputs
+ * of the tokens whose K rows the label cache is then built from.  DEVICE pointers.
+ * Sequences are packed: the new tokens of sequence s are rows [q_start[s], q_start[s + 1]) of q and
+ * out (q_start [n_seqs + 1] int32, ascending).  With nq of them and nk keys, of which the last nq are
+ * the new tokens' own,
+ *   out[i, hq] = sum_j softmax_j(q[i, hq] . k_j / sqrt(d)) v_j,   j <= i + nk - nq,   KV head hq / G
+ * for i = 0 .. nq - 1.  A row that sees no key (i + nk - nq < 0) is written as zero.  Rows of out outside
+ * every sequence are left as they are.
+ *   ds_prompt_attention: kv_start, kv_len [n_seqs] int32; key t of sequence s and KV head h is the row of
+ *     d elements at K + (kv_start[s] + t) * kv_stride + h * kv_head_stride, its value at V + the same.
+ *     So K and V may be packed like q (kv_start = q_start), parts of one fused projection, or the
+ *     contiguous caches above (kv_stride = d, kv_head_stride = L_max * d, kv_start[b] = b * Hkv * L_max;
+ *     DS_KV_INTERLEAVED: twice these strides, V = K + d elements).
+ *     kv_elems: elements from K (and from V) that may be read.
+ *   ds_prompt_attention_paged: the keys are the first lens[row] tokens of page table row rows[s] (rows NULL:
+ *     row s); see ds_pages_t.  prm->kv_stride, kv_head_stride and kv_elems are not used.
+ * Accumulation and softmax statistics are binary32; the weights are rounded once to the type of V, outputs
+ * once to the type of q.
+ * Argument checks: strides are multiples of 8 elements (0: the dense value, Hq * d for q and out, Hkv * d
+ * and d for kv_stride and kv_head_stride); q, K, V and out 16-byte aligned, pools of pages 256-byte.
+ * n_seqs < 1, total_q < 0, max_kv < 0, bad heads, d != 128, a stride below the row it steps over or
+ * beyond 2^30 (kv_head_stride: 2^40), an unknown dtype, or (total_q / 128 + n_seqs) * Hq beyond 2^24 -> DS_ERR_SHAPE.  What is on the device is checked there: a
+ * sequence whose new tokens do not lie in [0, total_q) is not computed (its rows are left as they are), one
+ * whose keys do not lie within kv_elems, within its row of the page table or on pages of the pool
+ * gets NaN, and nothing is read outside.
+ * max_kv: keys of the longest sequence (a guide to the split, which the results do not rest on).
+ */
+typedef enum { DS_F16 = 0, DS_BF16 = 1 } ds_dtype_t; /* IEEE binary16; bfloat16 */
+
+typedef struct {
+    int32_t n_seqs, Hq, Hkv, d;   /* sequences, query heads, KV heads, head dim (=128) */
+    int32_t total_q;              /* rows of q and out                                 */
+    int32_t max_kv;               /* keys of the longest sequence                      */
+    int32_t dtype;                /* ds_dtype_t of q, K, V and out                     */
+    int32_t reserved;             /* 0                                                 */
+    int64_t q_stride, out_stride; /* elements from token to token (0: Hq * d)          */
+    int64_t kv_stride, kv_head_stride; /* elements from token to token, head to head    */
+    int64_t kv_elems;             /* elements of K and of V that may be read           */
+} ds_prompt_t;
+
+/*
+ * Paged caches.  A pool (one of K and one of V for each layer) is [n_pages, Hkv, page_tokens, d]; a sequence
+ * is a row of the page table, table [n_rows, max_pages] int32: its token t lies in page
+ * table[row, t / page_tokens], place t % page_tokens, for t < lens[row] (lens [n_rows] int32).  Entries past
+ * the last page are not read.  All layers share table and lens.  Rows of a page past the last token may hold anything.
+ * page_tokens: 16, 32, 64, 128 or 256.  1 <= n_pages <= 2^20, 1 <= n_rows <= 65536, max_pages * page_tokens < 2^31,
+ * else DS_ERR_SHAPE.  Pools 256-byte aligned.
+ */
+typedef struct {
+    int32_t n_pages, page_tokens, Hkv, d; /* pages of a pool, tokens of a page, KV heads, head dim (=128) */
+    int32_t n_rows, max_pages;            /* rows of the page table, entries of a row                    */
+    int32_t dtype, reserved;              /* ds_dtype_t of the pools; 0                                  */
+} ds_pages_t;
+
+/* Bytes of workspace that a prompt call needs (a multiple of 256; cleared once with ds_workspace_init like
+ * every workspace).  Pure host function; 0 if the shape is invalid. */
+size_t ds_prompt_workspace_bytes(const ds_prompt_t *prm);
+ds_status_t ds_prompt_attention(const void *q, const void *K, const void *V, void *out,
+                                const int32_t *q_start, const int32_t *kv_start, const int32_t *kv_len,
+                                void *workspace, size_t workspace_bytes, const ds_prompt_t *prm, void *stream);
+ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const void *V_pages, void *out,
+                                      const int32_t *q_start, const int32_t *rows, const int32_t *lens,
+                                      const int32_t *table, void *workspace, size_t workspace_bytes,
+                                      const ds_prompt_t *prm, const ds_pages_t *pages, void *stream);
+
+/*
  * Measurement aids (not part of the method).
  * ds_probe_stream_read: one pass of plain 16-byte loads over `bytes` bytes of
  *   device memory (bytes % 16 == 0), xor-folded into sink[0..1023] (uint32,

@@ -20,6 +20,7 @@ DS_OK = 0
 DS_ERR_NULL, DS_ERR_SHAPE, DS_ERR_ALIGN, DS_ERR_WORKSPACE, DS_ERR_UNSUPPORTED, DS_ERR_HIP = -1, -2, -3, -4, -5, -6
 DS_CALIB_Q, DS_CALIB_K, DS_CALIB_QK = 0, 1, 2
 DS_KV_SPLIT, DS_KV_INTERLEAVED = 0, 1
+DS_F16, DS_BF16 = 0, 1
 
 EXPORTS = [
     "ds_strerror", "ds_version", "ds_calibrate_channels", "ds_build_label", "ds_append_label",
@@ -30,11 +31,22 @@ EXPORTS = [
     "ds_gather_rows_host", "ds_attend_rows", "ds_probe_stream_read", "ds_profile_kernel_count",
     "ds_profile_kernel_name", "ds_profile_enable", "ds_profile_reset", "ds_profile_read",
     "ds_tune_set", "ds_tune_get", "ds_plan_describe", "ds_pretend_device",
+    "ds_prompt_workspace_bytes", "ds_prompt_attention", "ds_prompt_attention_paged",
 ]
 
 
 class DsShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "L", "L_max", "r", "k")]
+
+
+class DsPrompt(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("n_seqs", "Hq", "Hkv", "d", "total_q", "max_kv", "dtype", "reserved")] +
+                [(n, ctypes.c_int64) for n in ("q_stride", "out_stride", "kv_stride", "kv_head_stride", "kv_elems")])
+
+
+class DsPages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_tokens", "Hkv", "d", "n_rows", "max_pages", "dtype",
+                                              "reserved")]
 
 
 class DsError(RuntimeError):
@@ -94,6 +106,11 @@ def lib() -> ctypes.CDLL:
         L.ds_tune_get.argtypes = [ctypes.c_int]
         L.ds_plan_describe.argtypes = [shp, i32, ctypes.POINTER(ctypes.c_int32)]
         L.ds_pretend_device.argtypes = [i32, i32, i32]
+        prm, pgs = ctypes.POINTER(DsPrompt), ctypes.POINTER(DsPages)
+        L.ds_prompt_workspace_bytes.restype = sz
+        L.ds_prompt_workspace_bytes.argtypes = [prm]
+        L.ds_prompt_attention.argtypes = [vp] * 8 + [sz, prm, vp]
+        L.ds_prompt_attention_paged.argtypes = [vp] * 9 + [sz, prm, pgs, vp]
         for name in EXPORTS:
             getattr(L, name)  # AttributeError names a missing export
         _lib = L
@@ -113,6 +130,16 @@ def shape(B, Hq, Hkv, d, L, L_max, r, k) -> DsShape:
     return DsShape(B, Hq, Hkv, d, L, L_max, r, k)
 
 
+def prompt(n_seqs, Hq, Hkv, d, total_q, max_kv, dtype=DS_F16, q_stride=0, out_stride=0, kv_stride=0, kv_head_stride=0,
+           kv_elems=0) -> DsPrompt:
+    return DsPrompt(n_seqs, Hq, Hkv, d, total_q, max_kv, dtype, 0, q_stride, out_stride, kv_stride, kv_head_stride,
+                    kv_elems)
+
+
+def pages(n_pages, page_tokens, Hkv, d, n_rows, max_pages, dtype=DS_F16) -> DsPages:
+    return DsPages(n_pages, page_tokens, Hkv, d, n_rows, max_pages, dtype, 0)
+
+
 def _dp(t):
     """Device (or pinned-host) pointer of a contiguous tensor, or NULL."""
     if t is None:
@@ -120,6 +147,24 @@ def _dp(t):
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _vp(t):
+    """Pointer of a tensor whose strides the call is told of, or NULL."""
+    return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def _bytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+def _cleared(n: int, where: str, device):
+    if n == 0:
+        raise DsError(DS_ERR_SHAPE, where)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ds_workspace_init(ws)
+    torch.cuda.current_stream(ws.device).synchronize()
+    return ws
 
 
 def _stream(stream=None):
@@ -322,3 +367,27 @@ def ds_plan_describe(shp: DsShape, label_kind: int = 0) -> dict:
 
 def ds_pretend_device(cus: int, xccs: int, lds_per_cu: int):
     _check(lib().ds_pretend_device(cus, xccs, lds_per_cu), "ds_pretend_device")
+
+
+def ds_prompt_workspace_bytes(prm: DsPrompt) -> int:
+    return int(lib().ds_prompt_workspace_bytes(ctypes.byref(prm)))
+
+
+def ds_prompt_workspace_alloc(prm: DsPrompt, device="cuda") -> "torch.Tensor":
+    """torch-allocated, cleared workspace for `prm`, as ds_workspace_alloc."""
+    return _cleared(ds_prompt_workspace_bytes(prm), "ds_prompt_workspace_bytes", device)
+
+
+def ds_prompt_attention(q, K, V, out, q_start, kv_start, kv_len, workspace, prm: DsPrompt, stream=None):
+    """q, K, V and out may be views with the strides that `prm` names."""
+    _check(lib().ds_prompt_attention(_vp(q), _vp(K), _vp(V), _vp(out), _dp(q_start), _dp(kv_start), _dp(kv_len),
+                                     _dp(workspace), _bytes(workspace), ctypes.byref(prm), _stream(stream)),
+           "ds_prompt_attention")
+
+
+def ds_prompt_attention_paged(q, K_pages, V_pages, out, q_start, rows, lens, table, workspace, prm: DsPrompt,
+                              pages: DsPages, stream=None):
+    _check(lib().ds_prompt_attention_paged(_vp(q), _dp(K_pages), _dp(V_pages), _vp(out), _dp(q_start), _dp(rows),
+                                           _dp(lens), _dp(table), _dp(workspace), _bytes(workspace),
+                                           ctypes.byref(prm), ctypes.byref(pages), _stream(stream)),
+           "ds_prompt_attention_paged")

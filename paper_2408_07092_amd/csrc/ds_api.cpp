@@ -393,7 +393,8 @@ bool make_dense_plan(const ds_shape_t &s, int n_tokens, DensePlan *p, size_t wor
 static const char *const kKernelNames[KID_COUNT] = {
     "k_init", "k_score", "k_cand", "k_attend", "k_compact", "k_dense",
     "k_attend_rows", "k_label", "k_gather_host", "k_probe",
-    "k_refine_attend", "k_append_kv", "k_q4_build", "k_q4_write", "k_predict_query", "k_q4_amax", "k_q4_code"};
+    "k_refine_attend", "k_append_kv", "k_q4_build", "k_q4_write", "k_predict_query", "k_q4_amax", "k_q4_code",
+    "k_prompt"};
 
 struct ProfRec { int id; hipEvent_t a, b; };
 static std::mutex g_prof_mu;
@@ -455,7 +456,7 @@ const char *ds_strerror(ds_status_t status)
     return "unknown status";
 }
 
-int ds_version(void) { return 112; }
+int ds_version(void) { return 200; }
 
 ds_status_t ds_calibrate_channels(const uint16_t *q_calib, const uint16_t *k_calib, int32_t N,
                                   int32_t Hq, int32_t Hkv, int32_t d, int32_t r,

@@ -1,0 +1,131 @@
+// C-ABI layer of prompt attention and of the paged cache: argument validation only; every device
+// step is enqueued through the launchers declared in ds_cache.h.
+#include <algorithm>
+#include <cstdint>
+
+#include <hip/hip_runtime.h>
+
+#include "ds_cache.h"
+
+using namespace ds;
+
+static bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+#define DS_TRY(expr)                                  \
+    do {                                              \
+        if ((expr) != hipSuccess) return DS_ERR_HIP;  \
+    } while (0)
+
+static bool heads_ok(int Hq, int Hkv, int d, int dtype)
+{
+    return Hq >= 1 && Hkv >= 1 && Hkv <= 65535 && Hq <= 65535 && Hq % Hkv == 0 && d == kD && (dtype == DS_F16 || dtype == DS_BF16);
+}
+
+// *m = *prm with the dense strides in the place of zeros
+static bool prompt_ok(const ds_prompt_t *prm, ds_prompt_t *m)
+{
+    *m = *prm;
+    if (m->n_seqs < 1 || m->total_q < 0 || m->max_kv < 0 || !heads_ok(m->Hq, m->Hkv, m->d, m->dtype)) return false;
+    const int64_t row = (int64_t)m->Hq * kD, most = 1ll << 30;
+    if (m->q_stride == 0) m->q_stride = row;
+    if (m->out_stride == 0) m->out_stride = row;
+    if (m->kv_stride == 0) m->kv_stride = (int64_t)m->Hkv * kD;
+    if (m->kv_head_stride == 0) m->kv_head_stride = kD;
+    for (int64_t s : {m->q_stride, m->out_stride, m->kv_stride, m->kv_head_stride})
+        if (s % 8 != 0) return false;
+    if (m->q_stride < row || m->out_stride < row || m->kv_stride < kD || m->kv_head_stride < kD || m->kv_elems < 0) return false;
+    if (m->q_stride > most || m->out_stride > most || m->kv_stride > most || m->kv_head_stride > 1ll << 40) return false;
+    // (a launch holds 2^32 threads at most, and rows are numbered in 32 bits)
+    return ((int64_t)m->total_q / kPromptRows + m->n_seqs) * m->Hq <= 1ll << 24;
+}
+
+static bool pages_ok(const ds_pages_t *p)
+{
+    if (p->page_tokens < 16 || p->page_tokens > 256 || (p->page_tokens & (p->page_tokens - 1))) return false;
+    if (p->n_pages < 1 || p->n_pages > 1 << 20 || p->n_rows < 1 || p->n_rows > 65536 || p->max_pages < 1) return false;
+    return (int64_t)p->max_pages * p->page_tokens < 1ll << 31 && heads_ok(p->Hkv, p->Hkv, p->d, p->dtype);
+}
+
+static int log2_of(int x) { return __builtin_ctz((unsigned)x); }
+
+extern "C" {
+
+size_t ds_prompt_workspace_bytes(const ds_prompt_t *prm)
+{
+    ds_prompt_t m;
+    PromptPlan p;
+    return prm && prompt_ok(prm, &m) && make_prompt_plan(m, &p) ? p.total : 0;
+}
+
+static PromptArgs prompt_args(const void *q, const void *K, const void *V, void *out, const int32_t *q_start,
+                              const int32_t *kv_len, const ds_prompt_t &m, const PromptPlan &p)
+{
+    PromptArgs a{};
+    a.q = q;
+    a.K = K;
+    a.V = V;
+    a.out = out;
+    a.q_start = q_start;
+    a.kv_len = kv_len;
+    a.q_stride = m.q_stride;
+    a.out_stride = m.out_stride;
+    a.kv_stride = m.kv_stride;
+    a.kv_head_stride = m.kv_head_stride;
+    a.kv_elems = m.kv_elems;
+    a.n_seqs = m.n_seqs;
+    a.Hkv = m.Hkv;
+    a.G = p.G;
+    a.total_q = m.total_q;
+    a.n_tiles = p.n_tiles;
+    return a;
+}
+
+ds_status_t ds_prompt_attention(const void *q, const void *K, const void *V, void *out, const int32_t *q_start,
+                                const int32_t *kv_start, const int32_t *kv_len, void *workspace,
+                                size_t workspace_bytes, const ds_prompt_t *prm, void *stream)
+{
+    if (!q || !K || !V || !out || !q_start || !kv_start || !kv_len || !workspace || !prm) return DS_ERR_NULL;
+    ds_prompt_t m;
+    PromptPlan p;
+    if (!prompt_ok(prm, &m)) return DS_ERR_SHAPE;
+    if (!make_prompt_plan(m, &p)) return DS_ERR_UNSUPPORTED;
+    if (!aligned(q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(workspace, 16) ||
+        !aligned(q_start, 4) || !aligned(kv_start, 4) || !aligned(kv_len, 4))
+        return DS_ERR_ALIGN;
+    if (workspace_bytes < p.total) return DS_ERR_WORKSPACE;
+    if (m.total_q == 0) return DS_OK;
+    PromptArgs a = prompt_args(q, K, V, out, q_start, kv_len, m, p);
+    a.kv_start = kv_start;
+    DS_TRY(launch_prompt(a, false, m.dtype, (hipStream_t)stream));
+    return DS_OK;
+}
+
+ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const void *V_pages, void *out,
+                                      const int32_t *q_start, const int32_t *rows, const int32_t *lens,
+                                      const int32_t *table, void *workspace, size_t workspace_bytes,
+                                      const ds_prompt_t *prm, const ds_pages_t *pages, void *stream)
+{
+    if (!q || !K_pages || !V_pages || !out || !q_start || !lens || !table || !workspace || !prm || !pages)
+        return DS_ERR_NULL;
+    ds_prompt_t m;
+    PromptPlan p;
+    if (!prompt_ok(prm, &m) || !pages_ok(pages)) return DS_ERR_SHAPE;
+    if (pages->Hkv != m.Hkv || pages->dtype != m.dtype || (!rows && m.n_seqs > pages->n_rows)) return DS_ERR_SHAPE;
+    if (!make_prompt_plan(m, &p)) return DS_ERR_UNSUPPORTED;
+    if (!aligned(q, 16) || !aligned(K_pages, 256) || !aligned(V_pages, 256) || !aligned(out, 16) ||
+        !aligned(workspace, 16) || !aligned(q_start, 4) || !aligned(rows, 4) || !aligned(lens, 4) || !aligned(table, 4))
+        return DS_ERR_ALIGN;
+    if (workspace_bytes < p.total) return DS_ERR_WORKSPACE;
+    if (m.total_q == 0) return DS_OK;
+    PromptArgs a = prompt_args(q, K_pages, V_pages, out, q_start, lens, m, p);
+    a.rows = rows;
+    a.table = table;
+    a.n_pages = pages->n_pages;
+    a.page_log2 = log2_of(pages->page_tokens);
+    a.max_pages = pages->max_pages;
+    a.n_table = pages->n_rows;
+    DS_TRY(launch_prompt(a, true, m.dtype, (hipStream_t)stream));
+    return DS_OK;
+}
+
+}  // extern "C"

@@ -57,6 +57,7 @@ enum KernelId {
     KID_PREDICT,
     KID_Q4_AMAX,
     KID_Q4_CODE,
+    KID_PROMPT,
     KID_COUNT
 };
 

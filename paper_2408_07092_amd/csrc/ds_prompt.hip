@@ -1,0 +1,277 @@
+// Attention over whole prompts: causal, grouped heads, packed sequences of unlike lengths, with the
+// keys in rows of any stride (packed, or the contiguous caches) or in pages.
+//
+//   O[i] = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(s_ij - m_i),   s_ij = log2(e)/sqrt(d) q_i . k_j
+//
+// over the keys j <= i + nk - nq, in one pass over the keys with a running maximum m and a
+// running sum.  Bound by the matrix units: 4 d flops a pair against a few bytes for each row.
+//
+// The G query heads of a KV head are rows of one matrix: row token * G + g.  A workgroup takes 128 of
+// these rows, a wavefront 32, and walks the keys in tiles of 64 that all of its wavefronts share from LDS.
+// Everything is computed transposed, so that a query row is a column and lives in one lane (and the
+// lane 32 away, which has the other half of the keys): its maximum, sum and rescaling are
+// scalars of the lane, and the weights come out of the first product in the layout that the
+// second one reads, with no exchange between lanes.
+//   S^T[key][row]  = K[key][:] . Q[row][:]          32x32x16, K from LDS, Q in registers
+//   O^T[ch][row]  += V^T[ch][key] . P^T[key][row]   32x32x16, V^T by transposing LDS reads
+// Lane roles (lo = lane % 32, hi = lane / 32): of S^T and O^T a lane holds column lo, and of each 32 rows
+// 8 (i / 4) + 4 hi + i % 4, i = 0..15.  As the second operand of P.V, eight keys of a lane are
+// 16 c + 4 hi + {0..3} and 16 c + 8 + 4 hi + {0..3}: the V^T operand is read in the same order.
+#include <algorithm>
+
+#include "ds_device.h"
+#include "ds_cache.h"
+
+namespace ds {
+
+constexpr float kPromptScale = 1.4426950408889634f * 0.08838834764831845f;  // log2(e) / sqrt(128)
+constexpr int kKeys = 64;                                  // keys of a tile
+constexpr int kTileBytes = kKeys * kD * 2;
+// The running maximum is raised only when a row's exceeds it by more than this (in the log2 domain), so
+// that most tiles rescale nothing; weights carry the factor 2^kRoom besides, which cancels in the quotient.  They
+// are at most 2^(7 + 8), within fp16, and normal fp16 numbers down to 2^-21 of the row's largest.
+constexpr float kSlack = 8.0f, kRoom = 7.0f;
+constexpr float kLeast = -1e30f;                           // stands for "no key yet": 2^(s - kLeast) is never formed
+
+template <class T>
+struct Mma;
+template <>
+struct Mma<_Float16> {
+    typedef half8 vec8;
+    typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f32x16 dot(vec8 a, vec8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mma<__bf16> {
+    typedef bf16x8 vec8;
+    typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ f32x16 dot(vec8 a, vec8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+
+// Where the 16-byte piece c of a tile's row r lies in LDS: rows of 256 bytes would put a column of
+// pieces on the same four banks.  K is read a piece of each of 32 rows at a time, V by the
+// transposing read two pieces of each of four rows.
+__device__ __forceinline__ int k_piece(int r, int c) { return r * 16 + (c ^ (r & 15)); }
+__device__ __forceinline__ int v_piece(int r, int c) { return r * 16 + (c ^ ((r & 3) << 2)); }
+
+__device__ __forceinline__ float halves_max(float v)
+{
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float halves_sum(float v)
+{
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+template <class T, bool PAGED>
+__global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
+{
+    typedef typename Mma<T>::vec8 vec8;
+    extern __shared__ __attribute__((aligned(16))) u32x4 tiles[];  // K, V, K, V: 16-byte pieces
+    constexpr int kPieces = kTileBytes / 16;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lo = lane & 31, hi = lane >> 5;
+    const int kvh = blockIdx.x % a.Hkv;
+    const int slot = a.n_tiles - 1 - (int)(blockIdx.x / a.Hkv);
+    // ---- the sequence and its rows
+    const int s = find_sequence(a.q_start, a.n_seqs, a.G, slot);
+    const int qs = a.q_start[s], qe = a.q_start[s + 1];
+    if (qs < 0 || qe < qs || qe > a.total_q) return;
+    const int n_rows = (qe - qs) * a.G;
+    const int r0 = (slot - tile_base(qs, a.G, s)) * kPromptRows;
+    if (r0 < 0 || r0 >= n_rows) return;
+    bool bad = false;
+    int nk;
+    int64_t kv0 = 0;
+    const int32_t *pages = nullptr;
+    if constexpr (PAGED) {
+        const int row = a.rows ? a.rows[s] : s;
+        bad = row < 0 || row >= a.n_table;
+        nk = bad ? 0 : a.kv_len[row];
+        pages = a.table + (size_t)(bad ? 0 : row) * a.max_pages;
+        bad |= nk < 0 || (int64_t)nk > (int64_t)a.max_pages << a.page_log2;
+    } else {
+        nk = a.kv_len[s];
+        kv0 = a.kv_start[s];
+        bad = nk < 0 || kv0 < 0 || (nk > 0 && (kv0 + nk - 1) * a.kv_stride + (int64_t)(a.Hkv - 1) * a.kv_head_stride + kD > a.kv_elems);
+        kv0 = kv0 * a.kv_stride + (int64_t)kvh * a.kv_head_stride;
+    }
+    if (bad) nk = 0;
+    const int before = nk - (qe - qs);               // keys ahead of the sequence's first row's own
+    const int last_row = min(n_rows, r0 + kPromptRows) - 1;
+    const int seen = max(0, min(nk, last_row / a.G + before + 1));    // keys that some row of the workgroup sees
+    const int n_kt = (seen + kKeys - 1) / kKeys;
+    const int my_row = r0 + wave * 32 + lo;
+    const bool on = my_row < n_rows;
+    const int my_last = on ? my_row / a.G + before : -1;              // last key that the lane's row sees
+    const int wave_first = (min(r0 + wave * 32, n_rows - 1)) / a.G + before;   // ... and the wavefront's first and last rows
+    const int wave_last = (min(r0 + wave * 32 + 31, n_rows - 1)) / a.G + before;
+
+    vec8 q[8];
+    {
+        const int row = min(my_row, n_rows - 1);
+        const T *src = static_cast<const T *>(a.q) + (size_t)(qs + row / a.G) * a.q_stride + (size_t)(kvh * a.G + row % a.G) * kD + hi * 8;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) q[x] = *reinterpret_cast<const vec8 *>(src + x * 16);
+    }
+    f32x16 O[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) O[d] = (f32x16)(0.0f);
+    float m = kLeast, l = 0.0f;
+
+    // ---- tiles: a thread moves piece tid % 16 of the rows tid / 16, + 16, ..; rows past the end re-read the last
+    constexpr int kPasses = kKeys * 16 / kWG;
+    u32x4 kr[kPasses], vr[kPasses];
+    auto load_tile = [&](int kt) {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int t = min(kt * kKeys + i * (kWG / 16) + tid / 16, nk - 1);
+            int64_t e;
+            if constexpr (PAGED) {
+                // (16 rows that start at a multiple of 16 are in one page)
+                int p = pages[t >> a.page_log2];
+                if ((uint32_t)p >= (uint32_t)a.n_pages) {
+                    bad = true;
+                    p = 0;
+                }
+                e = ((((int64_t)p * a.Hkv + kvh) << a.page_log2) + (t & ((1 << a.page_log2) - 1))) * kD;
+            } else {
+                e = kv0 + (int64_t)t * a.kv_stride;
+            }
+            kr[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.K) + e + (tid & 15) * 8);
+            vr[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.V) + e + (tid & 15) * 8);
+        }
+    };
+    auto store_tile = [&](int kt) {
+        u32x4 *kb = tiles + (kt & 1) * 2 * kPieces, *vb = kb + kPieces;
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int r = i * (kWG / 16) + tid / 16;
+            // (weight 0 times whatever lies behind the last key must be 0)
+            if (kt * kKeys + r >= nk) vr[i] = (u32x4)(0u);
+            kb[k_piece(r, tid & 15)] = kr[i];
+            vb[v_piece(r, tid & 15)] = vr[i];
+        }
+    };
+
+    if (n_kt > 0) {
+        load_tile(0);
+        store_tile(0);
+    }
+    __syncthreads();
+    for (int kt = 0; kt < n_kt; ++kt) {
+        const bool more = kt + 1 < n_kt;
+        if (more) load_tile(kt + 1);
+        if (kt * kKeys <= wave_last) {
+            const u32x4 *kb = tiles + (kt & 1) * 2 * kPieces, *vb = kb + kPieces;
+            f32x16 S[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                S[b] = (f32x16)(0.0f);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const vec8 k = __builtin_bit_cast(vec8, kb[k_piece(b * 32 + lo, 2 * x + hi)]);
+                    S[b] = Mma<T>::dot(k, q[x], S[b]);
+                }
+            }
+            // (only the tiles that hold the last keys of some row of the wavefront)
+            if (kt * kKeys + kKeys - 1 > min(wave_first, nk - 1)) {
+                const int left = min(my_last, nk - 1) - kt * kKeys - 4 * hi;
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (b * 32 + 8 * (i / 4) + i % 4 > left) S[b][i] = kNegInf;
+            }
+            float top = kNegInf;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, S[b][i]);
+            top = halves_max(top) * kPromptScale;
+            if (__any(top > m + kSlack)) {
+                const float mn = fmaxf(m, top);
+                const float f = __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) O[d] *= f;
+            }
+            const float shift = kRoom - m;
+            vec8 P[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[c / 2][8 * (c & 1) + j], kPromptScale, shift));
+                    l += p;
+                    P[c][j] = (T)p;  // (rounded once to the type of V; the sum is that of the weights before it)
+                }
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    // four keys by sixteen channels for each 16 lanes: lane 4 j + x brings row j, channels 4 x ..
+                    const int r = 16 * c + 4 * hi + (lane & 15) / 4, piece = d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2;
+                    const char *v0 = reinterpret_cast<const char *>(vb + v_piece(r, piece)) + (lane & 1) * 8;
+                    const char *v1 = reinterpret_cast<const char *>(vb + v_piece(r + 8, piece)) + (lane & 1) * 8;
+                    const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v0);
+                    const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v1);
+                    const s16x8 v = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+                    O[d] = Mma<T>::dot(__builtin_bit_cast(vec8, v), P[c], O[d]);
+                }
+        }
+        if (more) store_tile(kt + 1);
+        __syncthreads();
+    }
+    if constexpr (PAGED) {  // (a page that is not there: seen by the threads that would have read it)
+        uint32_t *flag = reinterpret_cast<uint32_t *>(tiles);
+        if (tid == 0) *flag = 0u;
+        __syncthreads();
+        if (bad) *flag = 1u;
+        __syncthreads();
+        bad = *flag != 0u;
+    }
+    if (!on) return;
+    l = halves_sum(l);
+    // (a row that sees no key is zero; one whose pages or places are not there is NaN)
+    const float inv = bad ? __builtin_nanf("") : l > 0.0f ? 1.0f / l : 0.0f;
+    T *dst = static_cast<T *>(a.out) + (size_t)(qs + my_row / a.G) * a.out_stride + (size_t)(kvh * a.G + my_row % a.G) * kD + 4 * hi;
+    typedef T vec4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            vec4 x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = (T)(O[d][4 * i + j] * inv);
+            *reinterpret_cast<vec4 *>(dst + d * 32 + i * 8) = x;
+        }
+}
+
+// ---------------------------------------------------------------- launcher
+bool make_prompt_plan(const ds_prompt_t &m, PromptPlan *p)
+{
+    p->G = m.Hq / m.Hkv;
+    p->n_tiles = (int)((int64_t)m.total_q * p->G / kPromptRows) + m.n_seqs;
+    p->total = 256;
+    return true;
+}
+
+typedef void (*PromptFn)(PromptArgs);
+static PromptFn prompt_fn(bool paged, int dtype)
+{
+    if (dtype == DS_BF16) return paged ? k_prompt<__bf16, true> : k_prompt<__bf16, false>;
+    return paged ? k_prompt<_Float16, true> : k_prompt<_Float16, false>;
+}
+
+hipError_t launch_prompt(PromptArgs a, bool paged, int dtype, hipStream_t st)
+{
+    const PromptFn fn = prompt_fn(paged, dtype);
+    DS_LAUNCH(KID_PROMPT, fn, dim3((unsigned)(a.n_tiles * a.Hkv)), dim3(kWG), 4 * kTileBytes, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace ds

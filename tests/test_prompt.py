@@ -1,0 +1,311 @@
+"""Attention over whole prompts: refusals on the host, and every layout, type and edge against the
+definition in 64 bits.
+
+Tolerance of an element y = sum p v / sum p, with A = sum p |v| / sum p and h = finfo(type).eps / 2, half a step:
+  h A        each weight is rounded once to the type of V (the sum of weights is of those before it)
+  h |y|      the output is rounded once
+  2 e A      a logit in binary32 is off by up to e = 130 * 2^-24 * sum |q||k| / sqrt(d) + 2^-20 (128 products summed, two
+             more roundings; the exponential): numerator and denominator both move by that share
+The largest e of a row's keys serves for the row."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2408_07092_amd as ds
+
+D = 128
+FAKE = ctypes.c_void_p(0x10000)   # aligned, never dereferenced: validation fails first
+TYPES = {"f16": (torch.float16, ds.DS_F16), "bf16": (torch.bfloat16, ds.DS_BF16)}
+
+
+# ------------------------------------------------------------------ host
+def call(prm, q=FAKE, K=FAKE, V=FAKE, out=FAKE, qs=FAKE, ks=FAKE, kl=FAKE, ws=FAKE, n=1 << 30):
+    return ds.lib().ds_prompt_attention(q, K, V, out, qs, ks, kl, ws, n, ctypes.byref(prm) if prm else None, None)
+
+
+def call_paged(prm, pg, q=FAKE, K=FAKE, V=FAKE, out=FAKE, qs=FAKE, rows=None, lens=FAKE, table=FAKE, ws=FAKE, n=1 << 30):
+    return ds.lib().ds_prompt_attention_paged(q, K, V, out, qs, rows, lens, table, ws, n, ctypes.byref(prm) if prm else None,
+                                              ctypes.byref(pg) if pg else None, None)
+
+
+GOOD = dict(n_seqs=3, Hq=8, Hkv=2, d=D, total_q=100, max_kv=50, kv_elems=1 << 20)
+
+
+def test_refusals():
+    ok = ds.prompt(**GOOD)
+    for name in ("q", "K", "V", "out", "qs", "ks", "kl", "ws"):
+        assert call(ok, **{name: None}) == ds.DS_ERR_NULL, name
+    assert call(None) == ds.DS_ERR_NULL
+    for bad in (dict(n_seqs=0), dict(total_q=-1), dict(max_kv=-1), dict(Hq=7), dict(Hkv=0), dict(Hq=0), dict(d=64), dict(dtype=2),
+                dict(dtype=-1), dict(q_stride=8 * D - 8), dict(q_stride=8 * D + 4), dict(out_stride=4), dict(kv_stride=120),
+                dict(kv_stride=D + 1), dict(kv_head_stride=8), dict(kv_elems=-1), dict(kv_stride=(1 << 30) + 8),
+                dict(q_stride=-8 * D), dict(kv_head_stride=(1 << 40) + 8), dict(total_q=2**31 - 1), dict(n_seqs=1 << 22)):
+        assert call(ds.prompt(**{**GOOD, **bad})) == ds.DS_ERR_SHAPE, bad
+        assert ds.ds_prompt_workspace_bytes(ds.prompt(**{**GOOD, **bad})) == 0
+    for name in ("q", "K", "V", "out", "ws"):
+        assert call(ok, **{name: ctypes.c_void_p(0x10008)}) == ds.DS_ERR_ALIGN, name
+    for name in ("qs", "ks", "kl"):
+        assert call(ok, **{name: ctypes.c_void_p(0x10002)}) == ds.DS_ERR_ALIGN, name
+    need = ds.ds_prompt_workspace_bytes(ok)
+    assert need > 0 and need % 256 == 0 and call(ok, n=need - 1) == ds.DS_ERR_WORKSPACE
+    assert call(ds.prompt(**{**GOOD, "total_q": 0})) == ds.DS_OK     # no rows: nothing to enqueue
+
+
+def test_paged_refusals():
+    ok, pg = ds.prompt(**GOOD), dict(n_pages=10, page_tokens=16, Hkv=2, d=D, n_rows=3, max_pages=4)
+    for name in ("q", "K", "V", "out", "qs", "lens", "table", "ws"):
+        assert call_paged(ok, ds.pages(**pg), **{name: None}) == ds.DS_ERR_NULL, name
+    assert call_paged(ok, None) == ds.DS_ERR_NULL and call_paged(None, ds.pages(**pg)) == ds.DS_ERR_NULL
+    for bad in (dict(page_tokens=8), dict(page_tokens=24), dict(page_tokens=512), dict(page_tokens=0), dict(page_tokens=-16),
+                dict(n_pages=0), dict(n_pages=(1 << 20) + 1), dict(Hkv=4), dict(d=64), dict(n_rows=0), dict(n_rows=65537),
+                dict(max_pages=0), dict(max_pages=1 << 27), dict(dtype=ds.DS_BF16), dict(dtype=7), dict(n_rows=2)):
+        assert call_paged(ok, ds.pages(**{**pg, **bad})) == ds.DS_ERR_SHAPE, bad
+    for name in ("K", "V"):
+        assert call_paged(ok, ds.pages(**pg), **{name: ctypes.c_void_p(0x10010)}) == ds.DS_ERR_ALIGN, name
+    for name in ("qs", "rows", "lens", "table"):
+        assert call_paged(ok, ds.pages(**pg), **{name: ctypes.c_void_p(0x10001)}) == ds.DS_ERR_ALIGN, name
+    assert call_paged(ok, ds.pages(**pg), n=ds.ds_prompt_workspace_bytes(ok) - 1) == ds.DS_ERR_WORKSPACE
+
+
+# ------------------------------------------------------------------ definition
+def defined(q, k, v, before):
+    """(y, A, e): q [m, Hq, d], k and v [t, Hkv, d], row i sees the keys up to i + before."""
+    m, Hq = q.shape[:2]
+    G = Hq // k.shape[1]
+    q, k, v = q.double().cpu(), k.double().cpu().repeat_interleave(G, 1), v.double().cpu().repeat_interleave(G, 1)
+    s = torch.einsum("mhd,thd->hmt", q, k) / math.sqrt(D)
+    size = torch.einsum("mhd,thd->hmt", q.abs(), k.abs()) / math.sqrt(D)
+    hidden = torch.arange(k.shape[0])[None, None] > torch.arange(m)[None, :, None] + before
+    s = s.masked_fill(hidden, -math.inf)
+    p = torch.exp(s - s.amax(2, keepdim=True).clamp(min=-1e300)) if k.shape[0] else s
+    total = p.sum(2, keepdim=True).clamp(min=1e-300)
+    y = torch.einsum("hmt,thd->mhd", p / total, v)
+    A = torch.einsum("hmt,thd->mhd", p / total, v.abs())
+    e = size.masked_fill(hidden, 0.0).amax(2) if k.shape[0] else torch.zeros(Hq, m, dtype=torch.double)
+    return y, A, (130 * 2.0**-24 * e + 2.0**-20).T[:, :, None]
+
+
+def near(got, q, k, v, before, dtype):
+    y, A, e = defined(q, k, v, before)
+    h = torch.finfo(dtype).eps / 2
+    tol = h * (A + y.abs()) + 2 * e * A + 1e-7
+    off = (got.double().cpu() - y).abs()
+    assert torch.isfinite(got).all() and (off <= tol).all(), f"off by {(off / tol).max():.3f} of the tolerance"
+
+
+def values(shape, dtype, seed, outliers=False):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g)
+    if outliers:
+        x[..., ::16] *= 8.0
+    return x.to(dtype)
+
+
+def starts(lengths, first=0):
+    return torch.tensor([first] + list(np.cumsum(lengths) + first), dtype=torch.int32)
+
+
+CANARY = -77.0
+
+# (new tokens of the sequences, keys before them): tile edges (rows of 128 / G tokens, 64 keys), sequences without a token
+# and without a key, more new tokens than keys, one token after many
+BATCHES = {
+    "one_token": ([1], [0]),
+    "one_after_many": ([1, 1], [700, 63]),
+    "edges": ([63, 64, 65, 128, 129, 1], [0, 0, 0, 0, 0, 0]),
+    "empties": ([0, 5, 0, 0, 70, 0], [0, 0, 9, 0, 0, 4]),
+    "fewer_keys": ([40, 200, 10], [-7, -130, -10]),
+    "parts": ([17, 100, 3, 33], [64, 1000, 127, 31]),
+    "long": ([1100], [0]),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(4, 4), (8, 2), (7, 1), (16, 1), (10, 2)], ids=str)
+@pytest.mark.parametrize("name", BATCHES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_packed_against_definition(dtype, name, heads):
+    t, code = TYPES[dtype]
+    (Hq, Hkv), (new, before) = heads, BATCHES[name]
+    keys = [a + b for a, b in zip(new, before)]
+    T, R = sum(new) + 5, sum(keys) + 9
+    q, K, V = values((T, Hq, D), t, 1).cuda(), values((R, Hkv, D), t, 2, True).cuda(), values((R, Hkv, D), t, 3).cuda()
+    V[sum(keys) + 2:] = math.nan        # behind the last sequence: never part of a result
+    K[sum(keys) + 2:] = math.inf
+    qs, ks = starts(new, 2), starts(keys, 2)
+    out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+    prm = ds.prompt(len(new), Hq, Hkv, D, T, max(keys), code, kv_elems=K.numel())
+    ws = ds.ds_prompt_workspace_alloc(prm)
+    ds.ds_prompt_attention(q, K, V, out, qs.cuda(), ks[:-1].contiguous().cuda(),
+                           torch.tensor(keys, dtype=torch.int32).cuda(), ws, prm)
+    torch.cuda.synchronize()
+    assert (out[:2] == CANARY).all() and (out[2 + sum(new):] == CANARY).all()
+    for i, (m, n, b) in enumerate(zip(new, keys, before)):
+        o, r = int(qs[i]), int(ks[i])
+        near(out[o:o + m], q[o:o + m], K[r:r + n], V[r:r + n], b, t)
+        if b < 0:
+            assert (out[o:o - b] == 0).all()      # rows that see no key
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("layout", ["fused", "cache", "interleaved"])
+def test_strided_layouts(layout, dtype):
+    t, code = TYPES[dtype]
+    Hq, Hkv, new, before = 12, 3, [70, 1, 33], [0, 50, 7] if layout != "fused" else [0, 0, 0]
+    keys = [a + b for a, b in zip(new, before)]
+    T, qs = sum(new), starts(new)
+    wide = values((T, Hq + 2 * Hkv + 1, D), t, 4).cuda()
+    out_wide = torch.full((T, Hq + 2, D), CANARY, dtype=t, device="cuda")
+    q, out = wide[:, :Hq], out_wide[:, 1:1 + Hq]
+    row = wide.stride(0)
+    if layout == "fused":
+        K, V, ks = wide[:, Hq:Hq + Hkv], wide[:, Hq + Hkv:Hq + 2 * Hkv], qs[:-1]
+        more = dict(kv_stride=row, kv_head_stride=D, kv_elems=(T - 1) * row + Hkv * D)
+        rows = [(K[a:a + n], V[a:a + n]) for a, n in zip(ks.tolist(), keys)]
+    else:
+        L_max = max(keys) + 3
+        inter = layout == "interleaved"
+        kv = torch.full((3, Hkv, L_max, 2, D), math.nan, dtype=t)
+        for i, n in enumerate(keys):
+            kv[i, :, :n] = values((Hkv, n, 2, D), t, 5 + i)
+        kv = kv.cuda()
+        K, V = (kv[:, :, :, 0], kv[:, :, :, 1]) if inter else (kv[:, :, :, 0].contiguous(), kv[:, :, :, 1].contiguous())
+        step = 2 if inter else 1
+        more = dict(kv_stride=D * step, kv_head_stride=L_max * D * step, kv_elems=kv.numel() - D if inter else K.numel())
+        ks = torch.arange(3, dtype=torch.int32) * Hkv * L_max
+        rows = [(K[i, :, :n].transpose(0, 1), V[i, :, :n].transpose(0, 1)) for i, n in enumerate(keys)]
+    prm = ds.prompt(3, Hq, Hkv, D, T, max(keys), code, q_stride=row, out_stride=out_wide.stride(0), **more)
+    ws = ds.ds_prompt_workspace_alloc(prm)
+    ds.ds_prompt_attention(q, K, V, out, qs.cuda(), ks.contiguous().cuda(), torch.tensor(keys, dtype=torch.int32).cuda(), ws, prm)
+    torch.cuda.synchronize()
+    assert (out_wide[:, 0] == CANARY).all() and (out_wide[:, -1] == CANARY).all()
+    for i, (k, v) in enumerate(rows):
+        near(out[int(qs[i]):int(qs[i + 1])], q[int(qs[i]):int(qs[i + 1])], k, v, before[i], t)
+
+
+def paged(keys, Hkv, P, t, seed, spare=3):
+    """Pools, table, and the keys and values of the sequences: pages in no order, NaN wherever nobody's rows are."""
+    held = [(n + P - 1) // P for n in keys]
+    n_pages = sum(held) + spare
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(seed))
+    table = torch.full((len(keys) + 2, max(held) + 2), -5, dtype=torch.int32)
+    pools = torch.full((2, n_pages, Hkv, P, D), math.nan, dtype=t)
+    kv, at = [], 0
+    for i, n in enumerate(keys):
+        x = values((2, n, Hkv, D), t, seed + 10 + i)
+        x[0, ..., ::16] *= 8
+        for j in range(held[i]):
+            part = x[:, j * P:(j + 1) * P].transpose(1, 2)
+            pools[:, order[at], :, :part.shape[2]] = part
+            table[i + 1, j] = order[at]
+            at += 1
+        kv.append(x)
+    return pools[0].contiguous().cuda(), pools[1].contiguous().cuda(), table.cuda(), kv
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("P", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_paged_against_definition(dtype, P):
+    t, code = TYPES[dtype]
+    Hq, Hkv = 8, 2
+    for name in ("one_after_many", "edges", "empties", "fewer_keys", "parts"):
+        new, before = BATCHES[name]
+        keys = [a + b for a, b in zip(new, before)]
+        Kp, Vp, table, kv = paged(keys, Hkv, P, t, 20)
+        T, qs = sum(new) + 1, starts(new)
+        q = values((T, Hq, D), t, 1).cuda()
+        lens = torch.tensor([999] + keys + [999], dtype=torch.int32).cuda()
+        rows = torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda()
+        out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+        prm = ds.prompt(len(new), Hq, Hkv, D, T, max(keys), code)
+        pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+        ws = ds.ds_prompt_workspace_alloc(prm)
+        ds.ds_prompt_attention_paged(q, Kp, Vp, out, qs.cuda(), rows, lens, table, ws, prm, pg)
+        torch.cuda.synchronize()
+        assert (out[-1] == CANARY).all()
+        for i, (m, b) in enumerate(zip(new, before)):
+            o = int(qs[i])
+            near(out[o:o + m], q[o:o + m], kv[i][0], kv[i][1], b, t)
+
+
+@pytest.mark.gpu
+def test_places_that_are_not_there():
+    """Sequences whose keys do not lie where they may be read give NaN, those whose rows do not are left alone,
+    and the others of the call do not notice."""
+    t, code, Hq, Hkv, P, new = torch.float16, ds.DS_F16, 4, 2, 16, [5, 40, 3, 20]
+    q = values((sum(new), Hq, D), t, 1).cuda()
+    K, V = values((100, Hkv, D), t, 2).cuda(), values((100, Hkv, D), t, 3).cuda()
+    qs = starts(new)
+    for i, (start, n) in enumerate([(96, 5), (0, 101), (-1, 3), (2**31 - 1, 20)]):   # one row too far, too long, before, far
+        ks, kl = [0, 20, 7, 60], [5, 40, 3, 20]
+        ks[i], kl[i] = start, n
+        out = torch.full((sum(new), Hq, D), CANARY, dtype=t, device="cuda")
+        prm = ds.prompt(4, Hq, Hkv, D, sum(new), 101, code, kv_elems=K.numel())
+        ds.ds_prompt_attention(q, K, V, out, qs.cuda(), torch.tensor(ks, dtype=torch.int32).cuda(),
+                               torch.tensor(kl, dtype=torch.int32).cuda(), ds.ds_prompt_workspace_alloc(prm), prm)
+        torch.cuda.synchronize()
+        for j in range(4):
+            o = slice(int(qs[j]), int(qs[j + 1]))
+            if j == i:
+                assert torch.isnan(out[o]).all()
+            else:
+                near(out[o], q[o], K[ks[j]:ks[j] + kl[j]], V[ks[j]:ks[j] + kl[j]], kl[j] - new[j], t)
+    # rows of q outside [0, total_q): not computed
+    for broken in ([-3, 5, 45, 48, 68], [0, 5, 45, 48, 69], [0, 5, 4, 48, 68]):
+        out = torch.full((sum(new), Hq, D), CANARY, dtype=t, device="cuda")
+        prm = ds.prompt(4, Hq, Hkv, D, sum(new), 40, code, kv_elems=K.numel())
+        ds.ds_prompt_attention(q, K, V, out, torch.tensor(broken, dtype=torch.int32).cuda(),
+                               torch.tensor([0, 20, 7, 60], dtype=torch.int32).cuda(), torch.tensor([5, 40, 3, 20], dtype=torch.int32).cuda(),
+                               ds.ds_prompt_workspace_alloc(prm), prm)
+        torch.cuda.synchronize()
+        bad = [i for i in range(4) if not 0 <= broken[i] <= broken[i + 1] <= sum(new)]
+        good = [r for i in range(4) if i not in bad for r in range(broken[i], broken[i + 1])]
+        left = sorted(set(range(sum(new))) - set(good))
+        assert bad and (out[left] == CANARY).all()
+    keys = [a + 30 for a in new]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 20)
+    held = torch.tensor(keys, dtype=torch.int32)
+    for i, (row, n, entry) in enumerate([(99, None, None), (None, 2**30, None), (None, None, Kp.shape[0]), (None, None, -1), (-1, None, None), (None, -1, None)]):
+        i %= 4
+        tb, rows, lens = table.clone(), torch.arange(1, 5, dtype=torch.int32), torch.cat((held[:1], held, held[:1]))
+        if row is not None:
+            rows[i] = row
+        if n is not None:
+            lens[i + 1] = n
+        if entry is not None:
+            tb[i + 1, (keys[i] - 1) // P] = entry
+        out = torch.full((sum(new), Hq, D), CANARY, dtype=t, device="cuda")
+        prm = ds.prompt(4, Hq, Hkv, D, sum(new), max(keys), code)
+        pg = ds.pages(Kp.shape[0], P, Hkv, D, tb.shape[0], tb.shape[1], code)
+        ds.ds_prompt_attention_paged(q, Kp, Vp, out, qs.cuda(), rows.cuda(), lens.cuda(), tb, ds.ds_prompt_workspace_alloc(prm), prm, pg)
+        torch.cuda.synchronize()
+        for j in range(4):
+            o = slice(int(qs[j]), int(qs[j + 1]))
+            if j == i:
+                assert torch.isnan(out[o]).any(dim=(1, 2)).any()
+                assert row is None and n is None or torch.isnan(out[o]).all()
+            else:
+                near(out[o], q[o], kv[j][0], kv[j][1], 30, t)
+
+
+@pytest.mark.gpu
+def test_extreme_weights():
+    """Logits far apart, a maximum that rises late and by little and by much, and equal logits over many keys."""
+    for t, code in TYPES.values():
+        q = torch.zeros((40, 2, D), dtype=t)
+        q[:, :, 0] = 30.0
+        K, V = torch.zeros((600, 1, D), dtype=t), values((600, 1, D), t, 3)
+        K[:, 0, 0] = torch.cat((torch.linspace(-200, 0, 300), torch.linspace(0, 3, 150), torch.full((100,), 3.0), torch.linspace(3, 200, 50))).to(t)
+        q[1::2, 1, 0] = 0.0
+        qs, kl = starts([40]), torch.tensor([600], dtype=torch.int32)
+        out = torch.zeros_like(q).cuda()
+        prm = ds.prompt(1, 2, 1, D, 40, 600, code, kv_elems=K.numel())
+        ds.ds_prompt_attention(q.cuda(), K.cuda(), V.cuda(), out, qs.cuda(), torch.zeros(1, dtype=torch.int32).cuda(), kl.cuda(),
+                               ds.ds_prompt_workspace_alloc(prm), prm)
+        torch.cuda.synchronize()
+        near(out, q, K, V, 560, t)
