@@ -383,6 +383,35 @@ ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const 
                                       const ds_prompt_t *prm, const ds_pages_t *pages, void *stream);
 
 /*
+ * Dense decode attention over a paged cache: ds_dense_decode for sequences of unlike lengths.  DEVICE pointers.
+ *   out[s, hq] = softmax(q[s, hq] . K^T / sqrt(d)) . V over the first lens[rows[s]] tokens of table row rows[s]
+ * q [n_seqs, Hq, d] of the pools' type, out [n_seqs, Hq, d] fp32, rows [n_seqs] int32 (NULL: sequence s is row s).
+ * Lengths are read on the device, so a captured call follows them; max_len (>= 0) is the length that the launch
+ * and the workspace are sized for, a guide that the results do not rest on, but bits of a sum may.  A sequence without a token gives
+ * zeros; one whose row, length or pages cannot be gives NaN, and nothing is read outside the table and the pools.
+ * Pools 256-byte aligned, q, out and workspace 16-byte.  n_seqs, Hq < 1, bad heads, rows NULL with n_seqs > n_rows,
+ * or n_seqs * Hkv * ceil(G / 16) * ceil(max_pages * page_tokens / 64) beyond 2^31 -> DS_ERR_SHAPE.
+ */
+size_t ds_paged_workspace_bytes(const ds_pages_t *pages, int32_t n_seqs, int32_t Hq, int32_t max_len);
+ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pages, float *out,
+                            const int32_t *rows, const int32_t *lens, const int32_t *table, void *workspace,
+                            size_t workspace_bytes, const ds_pages_t *pages, int32_t n_seqs, int32_t Hq,
+                            int32_t max_len, void *stream);
+
+/*
+ * Writes new tokens' rows into their pages, one layer's pools: rows [new_start[s], new_start[s + 1]) of k_new and
+ * v_new (Hkv rows of d elements each, new_stride elements from token to token, 0: Hkv * d; 16-byte aligned,
+ * total_new of them) become tokens start[s], start[s] + 1, .. of table row rows[s] (NULL: row s).  new_start
+ * [n_seqs + 1], start [n_seqs] int32 on the device; start[s] < 0: nothing is written for s.  The pages have to be in the table
+ * (ds_pages_extend); what has no page of the pool is not written.  Rows are distinct.  total_new * ceil(Hkv / 8)
+ * at most 2^26, else DS_ERR_SHAPE.
+ */
+ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages, void *V_pages,
+                            const int32_t *new_start, const int32_t *rows, const int32_t *start,
+                            const int32_t *table, const ds_pages_t *pages, int32_t n_seqs, int32_t total_new,
+                            int64_t new_stride, void *stream);
+
+/*
  * Measurement aids (not part of the method).
  * ds_probe_stream_read: one pass of plain 16-byte loads over `bytes` bytes of
  *   device memory (bytes % 16 == 0), xor-folded into sink[0..1023] (uint32,

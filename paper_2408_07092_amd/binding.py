@@ -32,6 +32,7 @@ EXPORTS = [
     "ds_profile_kernel_name", "ds_profile_enable", "ds_profile_reset", "ds_profile_read",
     "ds_tune_set", "ds_tune_get", "ds_plan_describe", "ds_pretend_device",
     "ds_prompt_workspace_bytes", "ds_prompt_attention", "ds_prompt_attention_paged",
+    "ds_paged_workspace_bytes", "ds_paged_decode", "ds_append_paged",
 ]
 
 
@@ -111,6 +112,10 @@ def lib() -> ctypes.CDLL:
         L.ds_prompt_workspace_bytes.argtypes = [prm]
         L.ds_prompt_attention.argtypes = [vp] * 8 + [sz, prm, vp]
         L.ds_prompt_attention_paged.argtypes = [vp] * 9 + [sz, prm, pgs, vp]
+        L.ds_paged_workspace_bytes.restype = sz
+        L.ds_paged_workspace_bytes.argtypes = [pgs, i32, i32, i32]
+        L.ds_paged_decode.argtypes = [vp] * 8 + [sz, pgs, i32, i32, i32, vp]
+        L.ds_append_paged.argtypes = [vp] * 8 + [pgs, i32, i32, ctypes.c_int64, vp]
         for name in EXPORTS:
             getattr(L, name)  # AttributeError names a missing export
         _lib = L
@@ -391,3 +396,28 @@ def ds_prompt_attention_paged(q, K_pages, V_pages, out, q_start, rows, lens, tab
                                            _dp(lens), _dp(table), _dp(workspace), _bytes(workspace),
                                            ctypes.byref(prm), ctypes.byref(pages), _stream(stream)),
            "ds_prompt_attention_paged")
+
+
+def ds_paged_workspace_bytes(pages: DsPages, n_seqs: int, Hq: int, max_len: int) -> int:
+    return int(lib().ds_paged_workspace_bytes(ctypes.byref(pages), n_seqs, Hq, max_len))
+
+
+def ds_paged_workspace_alloc(pages: DsPages, n_seqs: int, Hq: int, max_len: int, device="cuda") -> "torch.Tensor":
+    """torch-allocated, cleared workspace of ds_paged_decode, as ds_workspace_alloc."""
+    return _cleared(ds_paged_workspace_bytes(pages, n_seqs, Hq, max_len), "ds_paged_workspace_bytes", device)
+
+
+def ds_paged_decode(q, K_pages, V_pages, out, rows, lens, table, workspace, pages: DsPages, n_seqs: int, Hq: int,
+                    max_len: int, stream=None):
+    _check(lib().ds_paged_decode(_dp(q), _dp(K_pages), _dp(V_pages), _dp(out), _dp(rows), _dp(lens), _dp(table),
+                                 _dp(workspace), _bytes(workspace), ctypes.byref(pages), n_seqs, Hq, max_len,
+                                 _stream(stream)), "ds_paged_decode")
+
+
+def ds_append_paged(k_new, v_new, K_pages, V_pages, new_start, rows, start, table, pages: DsPages, n_seqs: int,
+                    stream=None):
+    """k_new, v_new [total_new, Hkv, d], dense or views that step the same from token to token."""
+    assert k_new.shape[0] == v_new.shape[0] and k_new.stride() == v_new.stride() and k_new.stride()[1:] == (pages.d, 1)
+    _check(lib().ds_append_paged(_vp(k_new), _vp(v_new), _dp(K_pages), _dp(V_pages), _dp(new_start), _dp(rows),
+                                 _dp(start), _dp(table), ctypes.byref(pages), n_seqs, k_new.shape[0], k_new.stride(0),
+                                 _stream(stream)), "ds_append_paged")

@@ -128,4 +128,91 @@ ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const 
     return DS_OK;
 }
 
+static bool paged_ok(const ds_pages_t *g, int32_t n_seqs, int32_t Hq, int32_t max_len)
+{
+    if (!pages_ok(g) || n_seqs < 1 || max_len < 0 || !heads_ok(Hq, g->Hkv, g->d, g->dtype)) return false;
+    const int64_t units = (int64_t)n_seqs * g->Hkv * ((Hq / g->Hkv + 15) / 16);
+    return units <= (1ll << 31) / (((int64_t)g->max_pages * g->page_tokens + kPiece - 1) / kPiece);
+}
+
+size_t ds_paged_workspace_bytes(const ds_pages_t *pages, int32_t n_seqs, int32_t Hq, int32_t max_len)
+{
+    if (!pages || !paged_ok(pages, n_seqs, Hq, max_len)) return 0;
+    PagedPlan p;
+    make_paged_plan(*pages, n_seqs, Hq, max_len, &p);
+    return p.total;
+}
+
+ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pages, float *out,
+                            const int32_t *rows, const int32_t *lens, const int32_t *table, void *workspace,
+                            size_t workspace_bytes, const ds_pages_t *pages, int32_t n_seqs, int32_t Hq,
+                            int32_t max_len, void *stream)
+{
+    if (!q || !K_pages || !V_pages || !out || !lens || !table || !workspace || !pages) return DS_ERR_NULL;
+    if (!paged_ok(pages, n_seqs, Hq, max_len) || (!rows && n_seqs > pages->n_rows)) return DS_ERR_SHAPE;
+    if (!aligned(q, 16) || !aligned(K_pages, 256) || !aligned(V_pages, 256) || !aligned(out, 16) ||
+        !aligned(workspace, 16) || !aligned(rows, 4) || !aligned(lens, 4) || !aligned(table, 4))
+        return DS_ERR_ALIGN;
+    PagedPlan p;
+    make_paged_plan(*pages, n_seqs, Hq, max_len, &p);
+    if (workspace_bytes < p.total) return DS_ERR_WORKSPACE;
+    PagedArgs a{};
+    a.q = q;
+    a.K = K_pages;
+    a.V = V_pages;
+    a.out = out;
+    a.arrived = static_cast<uint32_t *>(workspace);
+    a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.off_part);
+    a.rows = rows;
+    a.lens = lens;
+    a.table = table;
+    a.n = n_seqs;
+    a.Hkv = pages->Hkv;
+    a.G = p.G;
+    a.passes = p.passes;
+    a.least = p.least;
+    a.n_pages = pages->n_pages;
+    a.page_log2 = log2_of(pages->page_tokens);
+    a.max_pages = pages->max_pages;
+    a.n_table = pages->n_rows;
+    DS_TRY(launch_paged(a, p, pages->dtype, (hipStream_t)stream));
+    return DS_OK;
+}
+
+ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages, void *V_pages,
+                            const int32_t *new_start, const int32_t *rows, const int32_t *start,
+                            const int32_t *table, const ds_pages_t *pages, int32_t n_seqs, int32_t total_new,
+                            int64_t new_stride, void *stream)
+{
+    if (!k_new || !v_new || !K_pages || !V_pages || !new_start || !start || !table || !pages) return DS_ERR_NULL;
+    if (!pages_ok(pages) || n_seqs < 1 || total_new < 0 || (!rows && n_seqs > pages->n_rows)) return DS_ERR_SHAPE;
+    const int64_t row = (int64_t)pages->Hkv * kD;
+    if (new_stride == 0) new_stride = row;
+    if (new_stride < row || new_stride % 8 != 0 || new_stride > 1ll << 30) return DS_ERR_SHAPE;
+    if ((int64_t)total_new * ((pages->Hkv + 7) / 8) > 1ll << 26) return DS_ERR_SHAPE;
+    if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(K_pages, 256) || !aligned(V_pages, 256) ||
+        !aligned(new_start, 4) || !aligned(rows, 4) || !aligned(start, 4) || !aligned(table, 4))
+        return DS_ERR_ALIGN;
+    if (total_new == 0) return DS_OK;
+    AppendPagedArgs a{};
+    a.k_new = static_cast<const u32x4 *>(k_new);
+    a.v_new = static_cast<const u32x4 *>(v_new);
+    a.K = static_cast<u32x4 *>(K_pages);
+    a.V = static_cast<u32x4 *>(V_pages);
+    a.new_start = new_start;
+    a.rows = rows;
+    a.start = start;
+    a.table = table;
+    a.new_stride = new_stride / 8;
+    a.n = n_seqs;
+    a.total_new = total_new;
+    a.Hkv = pages->Hkv;
+    a.n_pages = pages->n_pages;
+    a.page_log2 = log2_of(pages->page_tokens);
+    a.max_pages = pages->max_pages;
+    a.n_table = pages->n_rows;
+    DS_TRY(launch_append_paged(a, (hipStream_t)stream));
+    return DS_OK;
+}
+
 }  // extern "C"

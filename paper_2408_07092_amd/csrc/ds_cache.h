@@ -15,6 +15,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------- prompt attention
 constexpr int kPromptRows = 128;   // rows (token * G + head of the group) of a workgroup
@@ -39,20 +40,49 @@ hipError_t launch_prompt(PromptArgs a, bool paged, int dtype, hipStream_t st);
 // floor(q_start[s] G / 128) + s on, which leaves room for the part tile that each one may end in.
 __device__ __forceinline__ int tile_base(int q_start, int G, int s) { return (int)((int64_t)q_start * G / kPromptRows) + s; }
 
-// The sequence whose tiles a number falls among, the last one that starts at or before it: 64 starts looked at at
-// a time, by every wavefront for itself.  (Starts that do not ascend give some sequence.)
-__device__ __forceinline__ int find_sequence(const int32_t *q_start, int n, int G, int slot)
+// The last i of [0, n) whose key is at or before x, keys ascending: 64 of them looked at at a time, by every
+// wavefront for itself (x the same in all lanes).  Keys that do not ascend give some i.
+template <class Key>
+__device__ __forceinline__ int last_at_or_before(int n, int x, Key key)
 {
     const int lane = threadIdx.x & 63;
     int first = 0, end = n;
     while (end - first > 1) {
         const int step = (end - first + 63) / 64, i = first + lane * step;
-        const bool before = i < end && tile_base(q_start[min(i, n - 1)], G, i) <= slot;
+        const bool before = i < end && key(min(i, n - 1)) <= x;
         const int k = __builtin_popcountll(__ballot(before));
         first += max(k - 1, 0) * step;
         end = min(end, first + step);
     }
     return first;
 }
+
+// ---------------------------------------------------------------- paged decode
+constexpr int kPiece = 64;         // tokens that a share is counted in: 16 for each wavefront of a workgroup
+
+struct PagedArgs {
+    const void *q, *K, *V;
+    float *out, *part;
+    uint32_t *arrived;             // per sequence and unit, zero between calls
+    const int32_t *rows, *lens, *table;
+    int n, Hkv, G, passes, least;  // passes of 16 heads over a KV head's rows; least pieces of a share
+    int n_pages, page_log2, max_pages, n_table;
+};
+struct PagedPlan {
+    int G, passes, GH, least, wgs;
+    size_t off_part, total;
+};
+void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan *p);
+hipError_t launch_paged(PagedArgs a, const PagedPlan &p, int dtype, hipStream_t st);
+
+struct AppendPagedArgs {
+    const u32x4 *k_new, *v_new;
+    u32x4 *K, *V;
+    const int32_t *new_start, *rows, *start, *table;
+    int64_t new_stride;            // 16-byte pieces from token to token
+    int n, total_new, Hkv;
+    int n_pages, page_log2, max_pages, n_table;
+};
+hipError_t launch_append_paged(const AppendPagedArgs &a, hipStream_t st);
 
 }  // namespace ds

@@ -58,6 +58,8 @@ enum KernelId {
     KID_Q4_AMAX,
     KID_Q4_CODE,
     KID_PROMPT,
+    KID_PAGED,
+    KID_APPEND_PAGED,
     KID_COUNT
 };
 

@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     const int kvh = blockIdx.x % a.Hkv;
     const int slot = a.n_tiles - 1 - (int)(blockIdx.x / a.Hkv);
     // ---- the sequence and its rows
-    const int s = find_sequence(a.q_start, a.n_seqs, a.G, slot);
+    const int s = last_at_or_before(a.n_seqs, slot, [&](int i) { return tile_base(a.q_start[i], a.G, i); });
     const int qs = a.q_start[s], qe = a.q_start[s + 1];
     if (qs < 0 || qe < qs || qe > a.total_q) return;
     const int n_rows = (qe - qs) * a.G;

@@ -1,0 +1,217 @@
+"""Attention of one new token over a paged cache and the writing of its pages' rows: refusals on the host, and
+lengths, pages, heads and types against the definition in 64 bits.
+
+Tolerance of an element y = sum p v / sum p over n tokens, with A = sum p |v| / sum p and h = finfo(type).eps / 2:
+  h^2 A                  a weight is the sum of two numbers of V's type, the second the rounded rest of the first
+  2 e A                  a logit is off by up to e = 130 * 2^-24 * sum |q||k| / sqrt(d) + 2^-20 (see test_prompt.py)
+  2 (n/4 + 300) 2^-24 A  sums in binary32: a wavefront adds every fourth 16 tokens, then states and parts are joined;
+                         numerator and denominator"""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2408_07092_amd as ds
+from test_prompt import CANARY, D, FAKE, TYPES, defined, paged, values
+
+
+# ------------------------------------------------------------------ host
+PG = dict(n_pages=10, page_tokens=16, Hkv=2, d=D, n_rows=3, max_pages=4)
+
+
+def decode(pg, n=3, Hq=4, max_len=60, q=FAKE, K=FAKE, V=FAKE, out=FAKE, rows=None, lens=FAKE, table=FAKE, ws=FAKE, nbytes=1 << 30):
+    return ds.lib().ds_paged_decode(q, K, V, out, rows, lens, table, ws, nbytes, ctypes.byref(pg) if pg else None, n, Hq, max_len, None)
+
+
+def append(pg, n=3, total=5, stride=0, k=FAKE, v=FAKE, K=FAKE, V=FAKE, new_start=FAKE, rows=None, start=FAKE, table=FAKE):
+    return ds.lib().ds_append_paged(k, v, K, V, new_start, rows, start, table, ctypes.byref(pg) if pg else None, n, total, stride, None)
+
+
+BAD_PAGES = (dict(page_tokens=8), dict(page_tokens=48), dict(page_tokens=512), dict(n_pages=0), dict(n_pages=(1 << 20) + 1),
+             dict(Hkv=0), dict(Hkv=-2), dict(d=64), dict(n_rows=0), dict(n_rows=65537), dict(max_pages=0), dict(max_pages=1 << 27),
+             dict(dtype=2), dict(dtype=-1))
+OFF = {16: ctypes.c_void_p(0x10008), 256: ctypes.c_void_p(0x10010), 4: ctypes.c_void_p(0x10002)}
+
+
+def test_decode_refusals():
+    ok = ds.pages(**PG)
+    for name in ("q", "K", "V", "out", "lens", "table", "ws"):
+        assert decode(ok, **{name: None}) == ds.DS_ERR_NULL, name
+    assert decode(None) == ds.DS_ERR_NULL
+    for bad in BAD_PAGES:
+        assert decode(ds.pages(**{**PG, **bad})) == ds.DS_ERR_SHAPE, bad
+        assert ds.ds_paged_workspace_bytes(ds.pages(**{**PG, **bad}), 3, 4, 60) == 0
+    for bad in (dict(n=0), dict(Hq=3), dict(Hq=0), dict(max_len=-1), dict(n=4)):   # (four sequences, three rows, no list of rows)
+        assert decode(ok, **bad) == ds.DS_ERR_SHAPE, bad
+    assert decode(ds.pages(**{**PG, "max_pages": 1 << 26}), n=3, Hq=704) == ds.DS_ERR_SHAPE   # 3 * 2 * 22 units of 2^24 pieces: beyond 2^31
+    for name, by in (("q", 16), ("out", 16), ("ws", 16), ("K", 256), ("V", 256), ("rows", 4), ("lens", 4), ("table", 4)):
+        assert decode(ok, **{name: OFF[by]}) == ds.DS_ERR_ALIGN, name
+    need = ds.ds_paged_workspace_bytes(ok, 3, 4, 60)
+    assert need > 0 and need % 256 == 0 and decode(ok, nbytes=need - 1) == ds.DS_ERR_WORKSPACE
+    assert ds.lib().ds_paged_workspace_bytes(None, 3, 4, 60) == 0
+
+
+def test_append_refusals():
+    ok = ds.pages(**PG)
+    for name in ("k", "v", "K", "V", "new_start", "start", "table"):
+        assert append(ok, **{name: None}) == ds.DS_ERR_NULL, name
+    assert append(None) == ds.DS_ERR_NULL
+    for bad in BAD_PAGES:
+        assert append(ds.pages(**{**PG, **bad})) == ds.DS_ERR_SHAPE, bad
+    for bad in (dict(n=0), dict(n=4), dict(total=-1), dict(stride=2 * D - 8), dict(stride=2 * D + 4), dict(stride=-2 * D),
+                dict(total=(1 << 26) + 1), dict(stride=(1 << 30) + 8)):
+        assert append(ok, **bad) == ds.DS_ERR_SHAPE, bad
+    for name, by in (("k", 16), ("v", 16), ("K", 256), ("V", 256), ("new_start", 4), ("rows", 4), ("start", 4), ("table", 4)):
+        assert append(ok, **{name: OFF[by]}) == ds.DS_ERR_ALIGN, name
+    assert append(ok, total=0) == ds.DS_OK
+
+
+# ------------------------------------------------------------------ decode
+def near(got, q, k, v, dtype):
+    n = k.shape[0]
+    y, A, e = defined(q[None], k, v, n - 1)
+    h = torch.finfo(dtype).eps / 2
+    tol = ((h * h + 2 * e + 2 * (n / 4 + 300) * 2.0**-24) * A + 1e-7)[0]
+    off = (got.double().cpu() - y[0]).abs()
+    assert torch.isfinite(got).all() and (off <= tol).all(), f"off by {(off / tol).max():.3f} of the tolerance"
+
+
+LENGTHS = {
+    "one": [1],
+    "short": [1, 15, 16, 17, 63, 64, 65, 127, 128, 129],
+    "ragged": [0, 3000, 1, 0, 0, 257, 40, 0],
+    "many": [(i * 37) % 90 for i in range(300)],      # more sequences than threads of a workgroup
+    "long": [20011, 5],
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(2, 2), (6, 2), (7, 1), (12, 1), (16, 1), (40, 2)], ids=str)   # groups of 1, 3, 7, 12, 16, 20
+@pytest.mark.parametrize("name", LENGTHS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decode_against_definition(dtype, name, heads):
+    t, code = TYPES[dtype]
+    (Hq, Hkv), keys = heads, LENGTHS[name]
+    P = {"one": 16, "short": 32, "ragged": 16, "many": 64, "long": 128}[name]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 30)
+    q = values((len(keys), Hq, D), t, 1).cuda()
+    lens = torch.tensor([7] + keys + [7], dtype=torch.int32).cuda()
+    rows = torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda()
+    out = torch.full((len(keys) + 2, Hq, D), CANARY, device="cuda")
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    ws = ds.ds_paged_workspace_alloc(pg, len(keys), Hq, max(keys))
+    for _ in range(2):       # (counters are zero again after a call)
+        ds.ds_paged_decode(q, Kp, Vp, out[1:-1], rows, lens, table, ws, pg, len(keys), Hq, max(keys))
+    torch.cuda.synchronize()
+    assert (out[0] == CANARY).all() and (out[-1] == CANARY).all()
+    for i, n in enumerate(keys):
+        if n == 0:
+            assert (out[i + 1] == 0).all()
+        else:
+            near(out[i + 1], q[i], kv[i][0], kv[i][1], t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("P", [16, 32, 64, 128, 256])
+def test_decode_page_sizes_and_a_wrong_guide(P):
+    """Pages of every size; a length to plan for that is far below or above the true ones changes no more than bits."""
+    t, code, keys, Hq, Hkv = torch.bfloat16, ds.DS_BF16, [P - 1, P, P + 1, 5 * P + 3, 1], 8, 2
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 31)
+    table, lens = table[1:-1].contiguous(), torch.tensor(keys, dtype=torch.int32).cuda()
+    q = values((len(keys), Hq, D), t, 1).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    for guide in (0, max(keys), 100 * max(keys)):
+        out = torch.full((len(keys), Hq, D), CANARY, device="cuda")
+        ds.ds_paged_decode(q, Kp, Vp, out, None, lens, table, ds.ds_paged_workspace_alloc(pg, len(keys), Hq, guide), pg, len(keys), Hq, guide)
+        torch.cuda.synchronize()
+        for i in range(len(keys)):
+            near(out[i], q[i], kv[i][0], kv[i][1], t)
+
+
+@pytest.mark.gpu
+def test_decode_places_that_are_not_there():
+    """A row, a length or a page that cannot be: NaN for that sequence, nothing else changes and nothing stays behind
+    in the workspace."""
+    t, code, P, Hq, Hkv, keys = torch.float16, ds.DS_F16, 16, 4, 2, [40, 700, 3, 90]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 32)
+    q = values((4, Hq, D), t, 1).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    ws = ds.ds_paged_workspace_alloc(pg, 4, Hq, 700)
+    good_rows, good_lens = torch.arange(1, 5, dtype=torch.int32), torch.tensor([1] + keys + [1], dtype=torch.int32)
+    for i, what in enumerate(("row", "before", "long", "page", "row_far", "negative", "page_before", "none")):
+        i %= 4
+        rows, lens, tb = good_rows.clone(), good_lens.clone(), table.clone()
+        if what in ("row", "row_far", "before"):
+            rows[i] = {"row": table.shape[0], "row_far": 2**31 - 1, "before": -1}[what]
+        if what in ("long", "negative"):
+            lens[i + 1] = {"long": table.shape[1] * P + 1, "negative": -5}[what]
+        if what in ("page", "page_before"):
+            tb[i + 1, (keys[i] - 1) // P // 2] = {"page": Kp.shape[0], "page_before": -1}[what]
+        out = torch.full((4, Hq, D), CANARY, device="cuda")
+        ds.ds_paged_decode(q, Kp, Vp, out, rows.cuda(), lens.cuda(), tb, ws, pg, 4, Hq, 700)
+        torch.cuda.synchronize()
+        for j in range(4):
+            if j == i and what != "none":
+                assert torch.isnan(out[j]).all(), what
+            else:
+                near(out[j], q[j], kv[j][0], kv[j][1], t)
+
+
+@pytest.mark.gpu
+def test_decode_beyond_32_bit_offsets():
+    """A pool of more than 4 GiB: pages at its far end are reached, by the decode, the prompt and the writing."""
+    t, code, P, Hkv, Hq, n = torch.float16, ds.DS_F16, 256, 8, 8, 300
+    n_pages = (1 << 32) // (P * Hkv * D * 2) + 64
+    Kp = torch.empty((n_pages, Hkv, P, D), dtype=t, device="cuda")
+    Vp = torch.empty_like(Kp)
+    table = torch.tensor([[n_pages - 1, n_pages - 2]], dtype=torch.int32).cuda()
+    lens = torch.tensor([n], dtype=torch.int32).cuda()
+    k, v, q = values((n, Hkv, D), t, 1), values((n, Hkv, D), t, 2), values((1, Hq, D), t, 3)
+    pg = ds.pages(n_pages, P, Hkv, D, 1, 2, code)
+    ds.ds_append_paged(k.cuda(), v.cuda(), Kp, Vp, torch.tensor([0, n], dtype=torch.int32).cuda(), None,
+                       torch.zeros(1, dtype=torch.int32).cuda(), table, pg, 1)
+    out = torch.zeros((1, Hq, D), device="cuda")
+    ds.ds_paged_decode(q.cuda(), Kp, Vp, out, None, lens, table, ds.ds_paged_workspace_alloc(pg, 1, Hq, n), pg, 1, Hq, n)
+    prm = ds.prompt(1, Hq, Hkv, D, 1, n, code)
+    out2 = torch.zeros((1, Hq, D), dtype=t, device="cuda")
+    ds.ds_prompt_attention_paged(q.cuda(), Kp, Vp, out2, torch.tensor([0, 1], dtype=torch.int32).cuda(), None, lens, table,
+                                 ds.ds_prompt_workspace_alloc(prm), prm, pg)
+    torch.cuda.synchronize()
+    near(out[0], q[0], k, v, t)
+    from test_prompt import near as near_prompt
+    near_prompt(out2, q, k, v, n - 1, t)
+
+
+# ------------------------------------------------------------------ append
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hkv", [1, 3, 8, 40])
+@pytest.mark.parametrize("P", [16, 64])
+def test_append(P, Hkv):
+    """Rows land where the table says, everything else of the pools stays; sequences without a place are passed over."""
+    t = torch.bfloat16
+    new, begin = [1, 0, 37, 5, 4, 2, 130], [15, 3, 0, 60, -1, 2 * 16 * 40, 7]
+    n, first, pages = len(new), 3, 40
+    T = sum(new) + first + 2
+    wide = values((T, 2 * Hkv + 1, D), t, 1).cuda()
+    k, v = wide[:, :Hkv], wide[:, Hkv:2 * Hkv]
+    order = torch.randperm(n * 12, generator=torch.Generator().manual_seed(2)).to(torch.int32).reshape(n, 12)
+    order[3, 4 if P == 16 else 1] = n * 12           # (that page is not one of the pool)
+    table = torch.full((n + 1, 12), -1, dtype=torch.int32)
+    rows = torch.tensor([2, 0, 1, 3, 4, 5, 7], dtype=torch.int32)
+    table = torch.full((8, 12), -1, dtype=torch.int32)
+    table[rows.long()] = order
+    new_start = torch.tensor([first] + [first + sum(new[:i + 1]) for i in range(n)], dtype=torch.int32)
+    pools = torch.randn((2, n * 12, Hkv, P, D), generator=torch.Generator().manual_seed(3)).to(t)
+    want = pools.clone()
+    for s in range(n):
+        for i in range(new[s]):
+            at = begin[s] + i
+            if begin[s] < 0 or at // P >= 12 or not 0 <= order[s, at // P] < n * 12:
+                continue
+            want[0, order[s, at // P], :, at % P] = k[new_start[s] + i].cpu()
+            want[1, order[s, at // P], :, at % P] = v[new_start[s] + i].cpu()
+    K, V = pools[0].contiguous().cuda(), pools[1].contiguous().cuda()
+    pg = ds.pages(n * 12, P, Hkv, D, 8, 12, ds.DS_BF16)
+    ds.ds_append_paged(k, v, K, V, new_start.cuda(), rows.cuda(), torch.tensor(begin, dtype=torch.int32).cuda(), table.cuda(), pg, n)
+    torch.cuda.synchronize()
+    assert torch.equal(K.cpu().view(torch.int16), want[0].view(torch.int16)) and torch.equal(V.cpu().view(torch.int16), want[1].view(torch.int16))
