@@ -412,6 +412,45 @@ ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages,
                             int64_t new_stride, void *stream);
 
 /*
+ * The books of a paged cache: which pages a row holds (table, lens) and how often a page is held (refs [n_pages]
+ * int32, 0 = free).  All of it is on the device and is read and changed there, so a captured step can take pages and give them
+ * back.  An empty cache is refs and lens zero.  Pages that are given out are the lowest free ones, ascending, in the
+ * order of the call's list.  Calls on the same books must not overlap.
+ * Each call writes *status (device): DS_PAGES_DONE, or what is wrong, and then nothing is changed but the outputs as said:
+ *   DS_PAGES_NO_ROOM  not enough free pages
+ *   DS_PAGES_LENGTH   a length that is negative or beyond max_pages * page_tokens, before or after
+ *   DS_PAGES_ROWS     a row that is none or is listed twice (fork: a destination listed twice, not empty, or a source too)
+ * Lists are int32 on the device, of 1 <= n <= 2048 rows (else DS_ERR_SHAPE).  refs 16-byte aligned, copies 16.
+ *   extend  row rows[i] grows by n_new[i] >= 0 tokens: gets ceil((len + n) / P) - ceil(len / P) pages.  start[i] = its length before,
+ *           or -1 where *status says that nothing was done (ds_append_paged then writes nothing for it).
+ *   fork    the empty row dst[i] becomes a second holder of src[i]'s tokens: its full pages are shared, for a
+ *           partly filled last page a free one is taken, so no row ever writes to a page that another holds.
+ *           copies[0 .. *n_copies) = {page, new page, tokens, 0}, in list order (room for n): to be copied in
+ *           every layer, see ds_pages_copy.  (*n_copies = 0 where nothing was done.)
+ *   free    the rows let go of their pages: entries -1, length 0.  A page whose count comes to 0 is free.
+ *   compact moves the n_live pages that are held to the front: those behind page n_live, ascending, to the free pages before
+ *           it, ascending; rewrites refs and the table.  copies as above (room for n_pages / 2; tokens = page_tokens).
+ *           Workspace of ds_pages_workspace_bytes() bytes, 16-byte aligned, which need not be cleared.
+ *   copy    one layer's pools, the first min(*n_copies, max_copies) entries: tokens [0, tokens) of `page`, K and V, to `new page`.
+ *           No page is both read and written (lists of one fork or compact call are such).  Entries with a page
+ *           that is none are passed over.  max_copies * Hkv * page_tokens at most 2^32.
+ */
+typedef enum { DS_PAGES_DONE = 0, DS_PAGES_NO_ROOM = 1, DS_PAGES_LENGTH = 2, DS_PAGES_ROWS = 3 } ds_pages_status_t;
+ds_status_t ds_pages_extend(int32_t *refs, int32_t *table, int32_t *lens, const int32_t *rows, const int32_t *n_new,
+                            int32_t *start, int32_t *status, const ds_pages_t *pages, int32_t n, void *stream);
+ds_status_t ds_pages_fork(int32_t *refs, int32_t *table, int32_t *lens, const int32_t *src, const int32_t *dst,
+                          int32_t *copies, int32_t *n_copies, int32_t *status, const ds_pages_t *pages, int32_t n,
+                          void *stream);
+ds_status_t ds_pages_free(int32_t *refs, int32_t *table, int32_t *lens, const int32_t *rows, int32_t *status,
+                          const ds_pages_t *pages, int32_t n, void *stream);
+size_t ds_pages_workspace_bytes(const ds_pages_t *pages);
+ds_status_t ds_pages_compact(int32_t *refs, int32_t *table, const int32_t *lens, int32_t *copies, int32_t *n_copies,
+                             int32_t *status, void *workspace, size_t workspace_bytes, const ds_pages_t *pages,
+                             void *stream);
+ds_status_t ds_pages_copy(void *K_pages, void *V_pages, const int32_t *copies, const int32_t *n_copies,
+                          const ds_pages_t *pages, int32_t max_copies, void *stream);
+
+/*
  * Measurement aids (not part of the method).
  * ds_probe_stream_read: one pass of plain 16-byte loads over `bytes` bytes of
  *   device memory (bytes % 16 == 0), xor-folded into sink[0..1023] (uint32,

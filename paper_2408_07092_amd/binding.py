@@ -21,6 +21,7 @@ DS_ERR_NULL, DS_ERR_SHAPE, DS_ERR_ALIGN, DS_ERR_WORKSPACE, DS_ERR_UNSUPPORTED, D
 DS_CALIB_Q, DS_CALIB_K, DS_CALIB_QK = 0, 1, 2
 DS_KV_SPLIT, DS_KV_INTERLEAVED = 0, 1
 DS_F16, DS_BF16 = 0, 1
+DS_PAGES_DONE, DS_PAGES_NO_ROOM, DS_PAGES_LENGTH, DS_PAGES_ROWS = 0, 1, 2, 3
 
 EXPORTS = [
     "ds_strerror", "ds_version", "ds_calibrate_channels", "ds_build_label", "ds_append_label",
@@ -33,6 +34,7 @@ EXPORTS = [
     "ds_tune_set", "ds_tune_get", "ds_plan_describe", "ds_pretend_device",
     "ds_prompt_workspace_bytes", "ds_prompt_attention", "ds_prompt_attention_paged",
     "ds_paged_workspace_bytes", "ds_paged_decode", "ds_append_paged",
+    "ds_pages_extend", "ds_pages_fork", "ds_pages_free", "ds_pages_workspace_bytes", "ds_pages_compact", "ds_pages_copy",
 ]
 
 
@@ -116,6 +118,13 @@ def lib() -> ctypes.CDLL:
         L.ds_paged_workspace_bytes.argtypes = [pgs, i32, i32, i32]
         L.ds_paged_decode.argtypes = [vp] * 8 + [sz, pgs, i32, i32, i32, vp]
         L.ds_append_paged.argtypes = [vp] * 8 + [pgs, i32, i32, ctypes.c_int64, vp]
+        L.ds_pages_extend.argtypes = [vp] * 7 + [pgs, i32, vp]
+        L.ds_pages_fork.argtypes = [vp] * 8 + [pgs, i32, vp]
+        L.ds_pages_free.argtypes = [vp] * 5 + [pgs, i32, vp]
+        L.ds_pages_workspace_bytes.restype = sz
+        L.ds_pages_workspace_bytes.argtypes = [pgs]
+        L.ds_pages_compact.argtypes = [vp] * 7 + [sz, pgs, vp]
+        L.ds_pages_copy.argtypes = [vp] * 4 + [pgs, i32, vp]
         for name in EXPORTS:
             getattr(L, name)  # AttributeError names a missing export
         _lib = L
@@ -421,3 +430,38 @@ def ds_append_paged(k_new, v_new, K_pages, V_pages, new_start, rows, start, tabl
     _check(lib().ds_append_paged(_vp(k_new), _vp(v_new), _dp(K_pages), _dp(V_pages), _dp(new_start), _dp(rows),
                                  _dp(start), _dp(table), ctypes.byref(pages), n_seqs, k_new.shape[0], k_new.stride(0),
                                  _stream(stream)), "ds_append_paged")
+
+
+def ds_pages_extend(refs, table, lens, rows, n_new, start, status, pages: DsPages, n: int, stream=None):
+    _check(lib().ds_pages_extend(_dp(refs), _dp(table), _dp(lens), _dp(rows), _dp(n_new), _dp(start), _dp(status),
+                                 ctypes.byref(pages), n, _stream(stream)), "ds_pages_extend")
+
+
+def ds_pages_fork(refs, table, lens, src, dst, copies, n_copies, status, pages: DsPages, n: int, stream=None):
+    _check(lib().ds_pages_fork(_dp(refs), _dp(table), _dp(lens), _dp(src), _dp(dst), _dp(copies), _dp(n_copies),
+                               _dp(status), ctypes.byref(pages), n, _stream(stream)), "ds_pages_fork")
+
+
+def ds_pages_free(refs, table, lens, rows, status, pages: DsPages, n: int, stream=None):
+    _check(lib().ds_pages_free(_dp(refs), _dp(table), _dp(lens), _dp(rows), _dp(status), ctypes.byref(pages), n,
+                               _stream(stream)), "ds_pages_free")
+
+
+def ds_pages_workspace_bytes(pages: DsPages) -> int:
+    return int(lib().ds_pages_workspace_bytes(ctypes.byref(pages)))
+
+
+def ds_pages_workspace_alloc(pages: DsPages, device="cuda") -> "torch.Tensor":
+    """torch-allocated workspace of ds_pages_compact."""
+    return _cleared(ds_pages_workspace_bytes(pages), "ds_pages_workspace_bytes", device)
+
+
+def ds_pages_compact(refs, table, lens, copies, n_copies, status, workspace, pages: DsPages, stream=None):
+    _check(lib().ds_pages_compact(_dp(refs), _dp(table), _dp(lens), _dp(copies), _dp(n_copies), _dp(status),
+                                  _dp(workspace), _bytes(workspace), ctypes.byref(pages), _stream(stream)),
+           "ds_pages_compact")
+
+
+def ds_pages_copy(K_pages, V_pages, copies, n_copies, pages: DsPages, max_copies: int, stream=None):
+    _check(lib().ds_pages_copy(_dp(K_pages), _dp(V_pages), _dp(copies), _dp(n_copies), ctypes.byref(pages), max_copies,
+                               _stream(stream)), "ds_pages_copy")

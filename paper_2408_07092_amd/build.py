@@ -12,7 +12,8 @@ LIB = os.path.join(HERE, "libdsattn.so")
 # the same library with the in-kernel stage stamps compiled in (bench.py --trace loads it)
 LIB_TRACE = os.path.join(HERE, "libdsattn_trace.so")
 SOURCES = ["ds_select.hip", "ds_attend.hip", "ds_misc.hip", "ds_decode_g1.hip", "ds_decode_g2.hip", "ds_decode_g4.hip",
-           "ds_decode_g8.hip", "ds_decode_g16.hip", "ds_prompt.hip", "ds_paged.hip", "ds_api.cpp", "ds_api_cache.cpp"]
+           "ds_decode_g8.hip", "ds_decode_g16.hip", "ds_prompt.hip", "ds_paged.hip", "ds_pages.hip",
+           "ds_api.cpp", "ds_api_cache.cpp"]
 HEADERS = ["ds_internal.h", "ds_device.h", "ds_attend_core.h", "ds_bins.h", "ds_decode_core.h", "ds_cache.h"]
 
 FLAGS = [

@@ -394,7 +394,7 @@ static const char *const kKernelNames[KID_COUNT] = {
     "k_init", "k_score", "k_cand", "k_attend", "k_compact", "k_dense",
     "k_attend_rows", "k_label", "k_gather_host", "k_probe",
     "k_refine_attend", "k_append_kv", "k_q4_build", "k_q4_write", "k_predict_query", "k_q4_amax", "k_q4_code",
-    "k_prompt", "k_paged", "k_append_paged"};
+    "k_prompt", "k_paged", "k_append_paged", "k_pages_extend", "k_pages_fork", "k_pages_free", "k_pages_compact", "k_pages_copy"};
 
 struct ProfRec { int id; hipEvent_t a, b; };
 static std::mutex g_prof_mu;

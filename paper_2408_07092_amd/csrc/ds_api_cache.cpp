@@ -215,4 +215,105 @@ ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages,
     return DS_OK;
 }
 
+// The books' arguments, checked; DS_OK and *a filled in.
+static ds_status_t books(int32_t *refs, int32_t *table, const int32_t *lens, const int32_t *rows, int32_t *status,
+                         const ds_pages_t *pages, int32_t n, PagesArgs *a)
+{
+    if (!refs || !table || !lens || !rows || !status || !pages) return DS_ERR_NULL;
+    if (!pages_ok(pages) || n < 1 || n > kPagesListed) return DS_ERR_SHAPE;
+    if (!aligned(refs, 16) || !aligned(table, 4) || !aligned(lens, 4) || !aligned(rows, 4) || !aligned(status, 4))
+        return DS_ERR_ALIGN;
+    *a = PagesArgs{};
+    a->refs = refs;
+    a->table = table;
+    a->lens = const_cast<int32_t *>(lens);
+    a->rows = rows;
+    a->status = status;
+    a->n = n;
+    a->n_pages = pages->n_pages;
+    a->page_log2 = log2_of(pages->page_tokens);
+    a->max_pages = pages->max_pages;
+    a->n_rows = pages->n_rows;
+    return DS_OK;
+}
+
+ds_status_t ds_pages_extend(int32_t *refs, int32_t *table, int32_t *lens, const int32_t *rows, const int32_t *n_new,
+                            int32_t *start, int32_t *status, const ds_pages_t *pages, int32_t n, void *stream)
+{
+    if (!n_new || !start) return DS_ERR_NULL;
+    PagesArgs a;
+    const ds_status_t rc = books(refs, table, lens, rows, status, pages, n, &a);
+    if (rc != DS_OK) return rc;
+    if (!aligned(n_new, 4) || !aligned(start, 4)) return DS_ERR_ALIGN;
+    a.n_new = n_new;
+    a.start = start;
+    DS_TRY(launch_pages_extend(a, (hipStream_t)stream));
+    return DS_OK;
+}
+
+ds_status_t ds_pages_fork(int32_t *refs, int32_t *table, int32_t *lens, const int32_t *src, const int32_t *dst,
+                          int32_t *copies, int32_t *n_copies, int32_t *status, const ds_pages_t *pages, int32_t n,
+                          void *stream)
+{
+    if (!dst || !copies || !n_copies) return DS_ERR_NULL;
+    PagesArgs a;
+    const ds_status_t rc = books(refs, table, lens, src, status, pages, n, &a);
+    if (rc != DS_OK) return rc;
+    if (!aligned(dst, 4) || !aligned(copies, 16) || !aligned(n_copies, 4)) return DS_ERR_ALIGN;
+    a.dst = dst;
+    a.copies = reinterpret_cast<int4 *>(copies);
+    a.n_copies = n_copies;
+    DS_TRY(launch_pages_fork(a, (hipStream_t)stream));
+    return DS_OK;
+}
+
+ds_status_t ds_pages_free(int32_t *refs, int32_t *table, int32_t *lens, const int32_t *rows, int32_t *status,
+                          const ds_pages_t *pages, int32_t n, void *stream)
+{
+    PagesArgs a;
+    const ds_status_t rc = books(refs, table, lens, rows, status, pages, n, &a);
+    if (rc != DS_OK) return rc;
+    DS_TRY(launch_pages_free(a, (hipStream_t)stream));
+    return DS_OK;
+}
+
+size_t ds_pages_workspace_bytes(const ds_pages_t *pages) { return pages && pages_ok(pages) ? pages_workspace(pages->n_pages) : 0; }
+
+ds_status_t ds_pages_compact(int32_t *refs, int32_t *table, const int32_t *lens, int32_t *copies, int32_t *n_copies,
+                             int32_t *status, void *workspace, size_t workspace_bytes, const ds_pages_t *pages,
+                             void *stream)
+{
+    if (!copies || !n_copies || !workspace) return DS_ERR_NULL;
+    PagesArgs a;
+    const ds_status_t rc = books(refs, table, lens, lens, status, pages, 1, &a);  // (there is no list of rows)
+    if (rc != DS_OK) return rc;
+    if (!aligned(copies, 16) || !aligned(n_copies, 4) || !aligned(workspace, 16)) return DS_ERR_ALIGN;
+    if (workspace_bytes < pages_workspace(pages->n_pages)) return DS_ERR_WORKSPACE;
+    a.copies = reinterpret_cast<int4 *>(copies);
+    a.n_copies = n_copies;
+    DS_TRY(launch_pages_compact(a, workspace, (hipStream_t)stream));
+    return DS_OK;
+}
+
+ds_status_t ds_pages_copy(void *K_pages, void *V_pages, const int32_t *copies, const int32_t *n_copies,
+                          const ds_pages_t *pages, int32_t max_copies, void *stream)
+{
+    if (!K_pages || !V_pages || !copies || !n_copies || !pages) return DS_ERR_NULL;
+    if (!pages_ok(pages) || max_copies < 0) return DS_ERR_SHAPE;
+    if ((int64_t)max_copies * pages->Hkv * pages->page_tokens > 1ll << 32) return DS_ERR_SHAPE;
+    if (!aligned(K_pages, 256) || !aligned(V_pages, 256) || !aligned(copies, 16) || !aligned(n_copies, 4)) return DS_ERR_ALIGN;
+    if (max_copies == 0) return DS_OK;
+    CopyPagesArgs a{};
+    a.K = static_cast<u32x4 *>(K_pages);
+    a.V = static_cast<u32x4 *>(V_pages);
+    a.copies = reinterpret_cast<const int4 *>(copies);
+    a.n_copies = n_copies;
+    a.max_copies = max_copies;
+    a.Hkv = pages->Hkv;
+    a.n_pages = pages->n_pages;
+    a.page_log2 = log2_of(pages->page_tokens);
+    DS_TRY(launch_pages_copy(a, (hipStream_t)stream));
+    return DS_OK;
+}
+
 }  // extern "C"

@@ -85,4 +85,29 @@ struct AppendPagedArgs {
 };
 hipError_t launch_append_paged(const AppendPagedArgs &a, hipStream_t st);
 
+// ---------------------------------------------------------------- the books of a paged cache
+constexpr int kPagesListed = 2048; // rows that a call may list
+
+struct PagesArgs {
+    int32_t *refs, *table, *lens;
+    const int32_t *rows;               // fork: the sources
+    const int32_t *n_new, *dst;        // extend; fork
+    int32_t *start;                    // extend
+    int4 *copies;                      // fork and compact: {from, to, tokens, 0}
+    int32_t *n_copies, *status;
+    int n, n_pages, page_log2, max_pages, n_rows;
+};
+struct CopyPagesArgs {
+    u32x4 *K, *V;
+    const int4 *copies;
+    const int32_t *n_copies;
+    int max_copies, Hkv, n_pages, page_log2;
+};
+hipError_t launch_pages_extend(const PagesArgs &a, hipStream_t st);
+hipError_t launch_pages_fork(const PagesArgs &a, hipStream_t st);
+hipError_t launch_pages_free(const PagesArgs &a, hipStream_t st);
+size_t pages_workspace(int n_pages);
+hipError_t launch_pages_compact(const PagesArgs &a, void *ws, hipStream_t st);
+hipError_t launch_pages_copy(const CopyPagesArgs &a, hipStream_t st);
+
 }  // namespace ds

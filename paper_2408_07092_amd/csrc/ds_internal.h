@@ -60,6 +60,11 @@ enum KernelId {
     KID_PROMPT,
     KID_PAGED,
     KID_APPEND_PAGED,
+    KID_PAGES_EXTEND,
+    KID_PAGES_FORK,
+    KID_PAGES_FREE,
+    KID_PAGES_COMPACT,
+    KID_PAGES_COPY,
     KID_COUNT
 };
 

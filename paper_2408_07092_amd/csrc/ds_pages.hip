@@ -1,0 +1,376 @@
+// The books of a paged cache, kept on the device so that a serving step that takes and gives back pages
+// can be captured: who holds which page (table, lens), and how often a page is held (refs, 0 = free).
+//
+// What is given out is always the lowest free pages, ascending, in the order of the call's list, so the
+// books follow from the calls alone and not from how they ran.  The counts themselves are the free list:
+// one workgroup looks through them, 16 K pages a round, until it has enough.  Its time is latency (a
+// round of loads, a scan over the workgroup, a few barriers); the copies of pages are what moves data.
+#include <algorithm>
+
+#include "ds_device.h"
+#include "ds_cache.h"
+
+namespace ds {
+
+constexpr int kBooks = 1024, kBookWaves = kBooks / 64;  // threads of the workgroup that keeps the books
+constexpr int kListed = kPagesListed / kBooks;          // list entries of a thread
+constexpr int kFound = 4096;                            // free pages that are remembered in LDS
+
+__device__ __forceinline__ int pages_in(const PagesArgs &a, int tokens) { return tokens > 0 ? ((tokens - 1) >> a.page_log2) + 1 : 0; }
+__device__ __forceinline__ bool length_ok(const PagesArgs &a, int64_t tokens) { return tokens >= 0 && tokens <= (int64_t)a.max_pages << a.page_log2; }
+
+struct BooksLds {
+    uint32_t seen[65536 / 32];        // a bit for every row
+    uint32_t w[kBookWaves];
+    uint32_t bad, got;
+};
+
+// Marks row r; whether it was marked already or is none.
+__device__ __forceinline__ bool mark(const PagesArgs &a, uint32_t *seen, int r)
+{
+    if (r < 0 || r >= a.n_rows) return true;
+    const uint32_t bit = 1u << (r & 31);
+    return (atomicOr(&seen[r >> 5], bit) & bit) != 0u;
+}
+
+// Goes through the free pages in ascending order, take(rank, page) for each, until `want` have been seen; how many
+// there are, or want if there are as many.  All threads of the workgroup call it.  take may write the
+// count of the page that it is given: a thread reads its 16 counts before it.
+template <class Take>
+__device__ __forceinline__ uint32_t each_free(const int32_t *refs, int n_pages, uint32_t want, uint32_t *s_w, Take take)
+{
+    uint32_t have = 0;
+    for (int p0 = 0; p0 < n_pages && have < want; p0 += kBooks * 16) {
+        const int mine = p0 + (int)threadIdx.x * 16;
+        uint32_t free = 0;
+        if (mine + 16 <= n_pages) {
+            typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+            i32x4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const i32x4 *>(refs + mine + 4 * i);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) free |= v[i][j] <= 0 ? 1u << (4 * i + j) : 0u;
+        } else {
+            for (int i = 0; i < 16 && mine + i < n_pages; ++i) free |= refs[mine + i] <= 0 ? 1u << i : 0u;
+        }
+        uint32_t total;
+        uint32_t rank = have + block_exclusive_scan<kBookWaves>((uint32_t)__builtin_popcount(free), s_w, &total);
+        for (; free && rank < want; free &= free - 1u, ++rank) take(rank, mine + __builtin_ctz(free));
+        have += total;
+    }
+    return min(have, want);
+}
+
+// Rows grow: see ds_pages_extend.
+__global__ __launch_bounds__(kBooks) void k_pages_extend(PagesArgs a)
+{
+    __shared__ BooksLds s;
+    __shared__ uint32_t first[kPagesListed];   // pages that the list's entries before this one need
+    __shared__ int32_t found[kFound];
+    const int tid = threadIdx.x;
+    for (int i = tid; i < 65536 / 32; i += kBooks) s.seen[i] = 0u;
+    if (tid == 0) s.bad = 0u;
+    __syncthreads();
+    int row[kListed], len[kListed], more[kListed];
+    uint32_t need[kListed], sum = 0;
+#pragma unroll
+    for (int k = 0; k < kListed; ++k) {
+        const int i = tid * kListed + k;
+        row[k] = len[k] = more[k] = 0;
+        need[k] = 0u;
+        if (i < a.n) {
+            row[k] = a.rows[i];
+            more[k] = a.n_new[i];
+            uint32_t code = mark(a, s.seen, row[k]) ? DS_PAGES_ROWS : 0;
+            if (code == 0) {
+                len[k] = a.lens[row[k]];
+                if (more[k] < 0 || !length_ok(a, len[k]) || !length_ok(a, (int64_t)len[k] + more[k])) code = DS_PAGES_LENGTH;
+            }
+            if (code) atomicMax(&s.bad, code);
+            else need[k] = min((uint32_t)(pages_in(a, len[k] + more[k]) - pages_in(a, len[k])), (uint32_t)a.n_pages + 1u);
+        }
+        sum += need[k];
+    }
+    uint32_t total;
+    uint32_t before = block_exclusive_scan<kBookWaves>(sum, s.w, &total);  // (2048 entries of 2^20 + 1 pages at most: no overflow)
+#pragma unroll
+    for (int k = 0; k < kListed; ++k) {
+        if (tid * kListed + k < a.n) first[tid * kListed + k] = before;
+        before += need[k];
+    }
+    __syncthreads();
+    uint32_t code = s.bad;
+    auto give = [&](uint32_t rank, int page) {
+        int lo = 0, hi = a.n;               // the last entry that starts at or before the rank: the one it belongs to
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (first[mid] <= rank) lo = mid;
+            else hi = mid;
+        }
+        const int r = a.rows[lo];
+        a.table[(size_t)r * a.max_pages + pages_in(a, a.lens[r]) + (rank - first[lo])] = page;
+        a.refs[page] = 1;
+    };
+    if (code == 0 && total > 0) {
+        if (total > (uint32_t)a.n_pages) {
+            code = DS_PAGES_NO_ROOM;
+        } else {
+            const uint32_t got = each_free(a.refs, a.n_pages, total, s.w, [&](uint32_t rank, int page) {
+                if (rank < kFound) found[rank] = page;
+            });
+            __syncthreads();
+            if (got < total) {
+                code = DS_PAGES_NO_ROOM;
+            } else if (total <= kFound) {
+                for (uint32_t rank = tid; rank < total; rank += kBooks) give(rank, found[rank]);
+            } else {
+                each_free(a.refs, a.n_pages, total, s.w, give);
+            }
+        }
+    }
+    __syncthreads();   // (give reads the lengths)
+#pragma unroll
+    for (int k = 0; k < kListed; ++k) {
+        const int i = tid * kListed + k;
+        if (i < a.n) {
+            a.start[i] = code ? -1 : len[k];
+            if (!code) a.lens[row[k]] = len[k] + more[k];
+        }
+    }
+    if (tid == 0) *a.status = (int32_t)code;
+}
+
+// dst shares src's full pages: wavefront w of n_waves takes every n_waves-th entry of the list.
+__device__ __forceinline__ void share_pages(const PagesArgs &a, int w, int n_waves)
+{
+    constexpr int kFlight = 4;
+    const int lane = threadIdx.x & 63;
+    for (int i = w; i < a.n; i += n_waves) {
+        const int32_t *from = a.table + (size_t)a.rows[i] * a.max_pages;
+        int32_t *to = a.table + (size_t)a.dst[i] * a.max_pages;
+        const int full = a.lens[a.rows[i]] >> a.page_log2;
+        for (int j0 = lane; j0 < full; j0 += 64 * kFlight) {
+            int p[kFlight];
+#pragma unroll
+            for (int k = 0; k < kFlight; ++k) p[k] = from[min(j0 + 64 * k, full - 1)];
+#pragma unroll
+            for (int k = 0; k < kFlight; ++k)
+                if (j0 + 64 * k < full) {
+                    to[j0 + 64 * k] = p[k];
+                    if ((uint32_t)p[k] < (uint32_t)a.n_pages) atomicAdd(&a.refs[p[k]], 1);
+                }
+        }
+    }
+}
+
+// Sequences branch: see ds_pages_fork.  rows: the sources.  share: the full pages too (else a launch of its own does them).
+__global__ __launch_bounds__(kBooks) void k_pages_fork(PagesArgs a, int share)
+{
+    __shared__ BooksLds s;
+    __shared__ int32_t found[kPagesListed];
+    const int tid = threadIdx.x;
+    for (int i = tid; i < 65536 / 32; i += kBooks) s.seen[i] = 0u;
+    if (tid == 0) s.bad = 0u;
+    __syncthreads();
+    int src[kListed], dst[kListed], len[kListed];
+    uint32_t half = 0;   // bit k: entry k's last page is partly filled
+#pragma unroll
+    for (int k = 0; k < kListed; ++k) {
+        const int i = tid * kListed + k;
+        src[k] = dst[k] = len[k] = 0;
+        if (i < a.n) {
+            src[k] = a.rows[i];
+            dst[k] = a.dst[i];
+            uint32_t code = src[k] < 0 || src[k] >= a.n_rows || mark(a, s.seen, dst[k]) ? DS_PAGES_ROWS : 0;
+            if (code == 0) {
+                len[k] = a.lens[src[k]];
+                if (a.lens[dst[k]] != 0) code = DS_PAGES_ROWS;
+                else if (!length_ok(a, len[k])) code = DS_PAGES_LENGTH;
+            }
+            if (code) atomicMax(&s.bad, code);
+            else if (len[k] & ((1 << a.page_log2) - 1)) half |= 1u << k;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kListed; ++k)   // a row that is branched is none that a branch goes to
+        if (tid * kListed + k < a.n && src[k] >= 0 && src[k] < a.n_rows && (s.seen[src[k] >> 5] >> (src[k] & 31) & 1u))
+            atomicMax(&s.bad, (uint32_t)DS_PAGES_ROWS);
+    uint32_t total;
+    uint32_t rank = block_exclusive_scan<kBookWaves>((uint32_t)__builtin_popcount(half), s.w, &total);
+    uint32_t code = s.bad;
+    if (code == 0 && total > 0) {
+        const uint32_t got = each_free(a.refs, a.n_pages, total, s.w, [&](uint32_t r, int page) { found[r] = page; });
+        if (got < total) code = DS_PAGES_NO_ROOM;
+    }
+    __syncthreads();
+    if (!code) {
+        // (lens of the branches come last: share_pages reads those of the sources, which are other rows)
+        if (share) share_pages(a, tid >> 6, kBookWaves);
+#pragma unroll
+        for (int k = 0; k < kListed; ++k)
+            if (tid * kListed + k < a.n) {
+                if (half >> k & 1u) {
+                    const int full = len[k] >> a.page_log2, page = found[rank];
+                    a.table[(size_t)dst[k] * a.max_pages + full] = page;
+                    a.refs[page] = 1;
+                    a.copies[rank] = make_int4(a.table[(size_t)src[k] * a.max_pages + full], page, len[k] & ((1 << a.page_log2) - 1), 0);
+                    ++rank;
+                }
+                a.lens[dst[k]] = len[k];
+            }
+    }
+    if (tid == 0) {
+        *a.n_copies = code ? 0 : (int32_t)total;
+        *a.status = (int32_t)code;
+    }
+}
+__global__ __launch_bounds__(kWG) void k_pages_share(PagesArgs a)
+{
+    if (*a.status == 0) share_pages(a, (int)(blockIdx.x * (kWG / 64) + (threadIdx.x >> 6)), (int)(gridDim.x * (kWG / 64)));
+}
+
+// Rows end: see ds_pages_free.  A workgroup for each row; each looks at the whole list, so that all agree on it.
+__global__ __launch_bounds__(kWG) void k_pages_free(PagesArgs a)
+{
+    __shared__ uint32_t seen[65536 / 32], s_bad;
+    const int tid = threadIdx.x;
+    for (int i = tid; i < (a.n_rows + 31) / 32; i += kWG) seen[i] = 0u;
+    if (tid == 0) s_bad = 0u;
+    __syncthreads();
+    for (int i = tid; i < a.n; i += kWG)
+        if (mark(a, seen, a.rows[i])) s_bad = 1u;
+    __syncthreads();
+    const bool bad = s_bad != 0u;
+    if (blockIdx.x == 0 && tid == 0) *a.status = bad ? DS_PAGES_ROWS : DS_PAGES_DONE;
+    if (bad) return;
+    const int row = a.rows[blockIdx.x];
+    const int held = min(pages_in(a, a.lens[row]), a.max_pages);
+    int32_t *entry = a.table + (size_t)row * a.max_pages;
+    for (int j = tid; j < held; j += kWG) {
+        const int p = entry[j];
+        if ((uint32_t)p < (uint32_t)a.n_pages) atomicSub(&a.refs[p], 1);
+        entry[j] = -1;
+    }
+    __syncthreads();
+    if (tid == 0) a.lens[row] = 0;
+}
+
+// The live pages behind the first n_live go to the free ones among them: see ds_pages_compact.  Leaves where every page went
+// in map.
+__global__ __launch_bounds__(kBooks) void k_pages_compact(PagesArgs a, int32_t *map, int32_t *holes)
+{
+    __shared__ uint32_t s_w[kBookWaves];
+    const int tid = threadIdx.x;
+    const uint32_t n_free = each_free(a.refs, a.n_pages, (uint32_t)a.n_pages, s_w, [](uint32_t, int) {});
+    const int n_live = a.n_pages - (int)n_free;
+    const uint32_t n_holes = each_free(a.refs, n_live, (uint32_t)n_live, s_w, [&](uint32_t rank, int page) { holes[rank] = page; });
+    __syncthreads();
+    // movers, ascending, meet the holes, ascending: as many of one as of the other
+    uint32_t have = 0;
+    for (int p0 = 0; p0 < a.n_pages; p0 += kBooks) {
+        const int p = p0 + tid;
+        const bool mover = p >= n_live && p < a.n_pages && a.refs[p] > 0;
+        uint32_t total = 0, rank = 0;
+        if (p0 + kBooks > n_live) {
+            rank = have + block_exclusive_scan<kBookWaves>(mover ? 1u : 0u, s_w, &total);
+            have += total;
+        }
+        int to = p;
+        if (mover) {
+            to = holes[rank];
+            a.copies[rank] = make_int4(p, to, 1 << a.page_log2, 0);
+            a.refs[to] = a.refs[p];
+            a.refs[p] = 0;
+        }
+        if (p < a.n_pages) map[p] = to;
+    }
+    if (tid == 0) {
+        *a.n_copies = (int32_t)n_holes;
+        *a.status = DS_PAGES_DONE;
+    }
+}
+__global__ __launch_bounds__(kWG) void k_pages_remap(PagesArgs a, const int32_t *map)
+{
+    const int row = blockIdx.x, held = min(pages_in(a, a.lens[row]), a.max_pages);
+    int32_t *entry = a.table + (size_t)row * a.max_pages;
+    for (int j = blockIdx.y * kWG + threadIdx.x; j < held; j += gridDim.y * kWG) {
+        const int p = entry[j];
+        if ((uint32_t)p < (uint32_t)a.n_pages) entry[j] = map[p];
+    }
+}
+
+// Copies the listed pages' rows, K's and V's: 16 lanes to a row of 256 bytes, a workgroup 64 rows of an entry at a
+// time.  Bound by memory, a read and a write of every row.
+__global__ __launch_bounds__(kWG) void k_pages_copy(CopyPagesArgs a)
+{
+    const int n = min(max(*a.n_copies, 0), a.max_copies), P = 1 << a.page_log2;
+    const int groups = (2 * a.Hkv * P) / 64;      // of 64 rows, in an entry (P is 16 or more and there are two pools ..
+    const int rest = (2 * a.Hkv * P) % 64;        // .. so what is left is 32 rows, or none)
+    const int per = groups + (rest ? 1 : 0);
+    const uint32_t all = (uint32_t)n * (uint32_t)per;   // (2^28 at most)
+    for (uint32_t w = blockIdx.x; w < all; w += gridDim.x) {
+        const int4 e = a.copies[w / (uint32_t)per];
+        if ((uint32_t)e.x >= (uint32_t)a.n_pages || (uint32_t)e.y >= (uint32_t)a.n_pages) continue;
+        const int r0 = (int)(w % (uint32_t)per) * 64 + (threadIdx.x >> 4);
+        u32x4 v[4];
+        size_t to[4];
+        bool on[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = r0 + 16 * k, x = r >> a.page_log2, t = r & (P - 1);   // x: head of K, then head of V
+            on[k] = x < 2 * a.Hkv && t < e.z;
+            const int h = x < a.Hkv ? x : x - a.Hkv;
+            const size_t in_page = (size_t)(h * P + t) * 16 + (threadIdx.x & 15), page = (size_t)a.Hkv * P * 16;
+            to[k] = e.y * page + in_page;
+            v[k] = (u32x4)(0u);
+            if (on[k]) v[k] = (x < a.Hkv ? a.K : a.V)[e.x * page + in_page];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (on[k]) ((r0 + 16 * k) >> a.page_log2 < a.Hkv ? a.K : a.V)[to[k]] = v[k];
+    }
+}
+
+// ---------------------------------------------------------------- launchers
+hipError_t launch_pages_extend(const PagesArgs &a, hipStream_t st)
+{
+    DS_LAUNCH(KID_PAGES_EXTEND, k_pages_extend, dim3(1), dim3(kBooks), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const PagesArgs &a, hipStream_t st)
+{
+    // One workgroup shares up to 16 rows of 256 entries in one step; more than a few of these are worth a launch.
+    const bool alone = (int64_t)a.n * a.max_pages <= 16384;
+    DS_LAUNCH(KID_PAGES_FORK, k_pages_fork, dim3(1), dim3(kBooks), 0, st, a, alone ? 1 : 0);
+    if (!alone) DS_LAUNCH(KID_PAGES_FORK, k_pages_share, dim3((a.n + kWG / 64 - 1) / (kWG / 64)), dim3(kWG), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_free(const PagesArgs &a, hipStream_t st)
+{
+    DS_LAUNCH(KID_PAGES_FREE, k_pages_free, dim3(a.n), dim3(kWG), 0, st, a);
+    return hipGetLastError();
+}
+
+size_t pages_workspace(int n_pages) { return ((size_t)n_pages * 2 * 4 + 255) / 256 * 256; }
+
+hipError_t launch_pages_compact(const PagesArgs &a, void *ws, hipStream_t st)
+{
+    auto *map = static_cast<int32_t *>(ws);
+    DS_LAUNCH(KID_PAGES_COMPACT, k_pages_compact, dim3(1), dim3(kBooks), 0, st, a, map, map + a.n_pages);
+    DS_LAUNCH(KID_PAGES_COMPACT, k_pages_remap, dim3(a.n_rows, std::min((a.max_pages + kWG - 1) / kWG, 64)), dim3(kWG), 0, st, a, map);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const CopyPagesArgs &a, hipStream_t st)
+{
+    const int64_t work = (int64_t)a.max_copies * (((2 * a.Hkv << a.page_log2) + 63) / 64);
+    DS_LAUNCH(KID_PAGES_COPY, k_pages_copy, dim3((unsigned)std::min<int64_t>(work, device_caps().cus * 8)), dim3(kWG), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace ds
