@@ -18,6 +18,7 @@
 // 8 (i / 4) + 4 hi + i % 4, i = 0..15.  As the second operand of P.V, eight keys of a lane are
 // 16 c + 4 hi + {0..3} and 16 c + 8 + 4 hi + {0..3}: the V^T operand is read in the same order.
 #include <algorithm>
+#include <type_traits>
 
 #include "ds_device.h"
 #include "ds_cache.h"
@@ -40,12 +41,14 @@ struct Mma<_Float16> {
     typedef half8 vec8;
     typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ f32x16 dot(vec8 a, vec8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float add2(vec2 p, float l) { return __builtin_amdgcn_fdot2(p, (vec2)(_Float16)1.0f, l, false); }
 };
 template <>
 struct Mma<__bf16> {
     typedef bf16x8 vec8;
     typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ f32x16 dot(vec8 a, vec8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float add2(vec2 p, float l) { return __builtin_amdgcn_fdot2_f32_bf16(p, (vec2)(__bf16)1.0f, l, false); }
 };
 
 // Where the 16-byte piece c of a tile's row r lies in LDS: rows of 256 bytes would put a column of
@@ -65,14 +68,28 @@ __device__ __forceinline__ float halves_sum(float v)
     return __uint_as_float(r.x) + __uint_as_float(r.y);
 }
 
+// Sixteen bytes of every lane from memory into LDS, to `at` (bytes, the wavefront's) + 16 lane, past the registers.
+// Written out because the compiler, not knowing which buffer a transposing read reads, would wait for every load
+// in flight ahead of each of them; the loads are waited for by wait_tiles.  (m0, the place in LDS, is used for nothing
+// else in this kernel.)
+__device__ __forceinline__ void load_to_lds(const void *src, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(at), "v"(src) : "memory");
+}
+__device__ __forceinline__ void wait_tiles()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 template <class T, bool PAGED>
 __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
 {
     typedef typename Mma<T>::vec8 vec8;
-    extern __shared__ __attribute__((aligned(16))) u32x4 tiles[];  // K, V, K, V: 16-byte pieces
+    extern __shared__ __attribute__((aligned(16))) u32x4 tiles[];  // K, K, V, V: 16-byte pieces
     constexpr int kPieces = kTileBytes / 16;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lo = lane & 31, hi = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 31, hi = lane >> 5;
     const int kvh = blockIdx.x % a.Hkv;
     const int slot = a.n_tiles - 1 - (int)(blockIdx.x / a.Hkv);
     // ---- the sequence and its rows
@@ -105,9 +122,10 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     const int n_kt = (seen + kKeys - 1) / kKeys;
     const int my_row = r0 + wave * 32 + lo;
     const bool on = my_row < n_rows;
-    const int my_last = on ? my_row / a.G + before : -1;              // last key that the lane's row sees
-    const int wave_first = (min(r0 + wave * 32, n_rows - 1)) / a.G + before;   // ... and the wavefront's first and last rows
-    const int wave_last = (min(r0 + wave * 32 + 31, n_rows - 1)) / a.G + before;
+    const int my_last = on ? min(my_row / a.G + before, nk - 1) : -1; // last key that the lane's row sees
+    // tiles that some row of the wavefront sees, and those that all of its rows see whole
+    const int n_mine = min(n_kt, max(0, (min(r0 + wave * 32 + 31, n_rows - 1)) / a.G + before + kKeys) / kKeys);
+    const int n_clear = r0 + wave * 32 >= n_rows ? 0 : max(0, min((r0 + wave * 32) / a.G + before + 1, nk)) / kKeys;
 
     vec8 q[8];
     {
@@ -121,110 +139,169 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     for (int d = 0; d < 4; ++d) O[d] = (f32x16)(0.0f);
     float m = kLeast, l = 0.0f;
 
-    // ---- tiles: a thread moves piece tid % 16 of the rows tid / 16, + 16, ..; rows past the end re-read the last
-    constexpr int kPasses = kKeys * 16 / kWG;
-    u32x4 kr[kPasses], vr[kPasses];
-    auto load_tile = [&](int kt) {
-#pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const int t = min(kt * kKeys + i * (kWG / 16) + tid / 16, nk - 1);
-            int64_t e;
-            if constexpr (PAGED) {
-                // (16 rows that start at a multiple of 16 are in one page)
-                int p = pages[t >> a.page_log2];
-                if ((uint32_t)p >= (uint32_t)a.n_pages) {
-                    bad = true;
-                    p = 0;
-                }
-                e = ((((int64_t)p * a.Hkv + kvh) << a.page_log2) + (t & ((1 << a.page_log2) - 1))) * kD;
-            } else {
-                e = kv0 + (int64_t)t * a.kv_stride;
+    // ---- tiles: of each 16 rows a wavefront brings four, a lane one piece.  The pieces of a row change places on the
+    // way (see k_piece), by the lane's place in memory, since in LDS a load's lanes lie side by side.
+    // Rows past the last key re-read it (their weight is 0, and 0 times whatever lies behind it need not be).
+    const int lane_row = 4 * wave + (lane >> 4);
+    const int64_t step_row = PAGED ? kD : a.kv_stride;
+    const T *Kp = static_cast<const T *>(a.K) + kv0 + lane_row * step_row + ((lane & 15) ^ lane_row) * 8;
+    const T *Vp = static_cast<const T *>(a.V) + kv0 + lane_row * step_row + ((lane & 15) ^ ((lane >> 4) << 2)) * 8;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)tiles + wave * 1024;
+    // Paged: lane i % 4 of `of` holds the page of a tile's rows 16 i .. (16 rows that start at a multiple of 16 are in one page)
+    auto page_ids = [&](int kt) {
+        int p = 0;
+        if constexpr (PAGED) {
+            if (nk > 0) p = pages[min(kt * kKeys + (lane & 3) * 16, nk - 1) >> a.page_log2];
+            if ((uint32_t)p >= (uint32_t)a.n_pages) {
+                if (kt < n_kt) bad = true;
+                p = 0;
             }
-            kr[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.K) + e + (tid & 15) * 8);
-            vr[i] = *reinterpret_cast<const u32x4 *>(static_cast<const T *>(a.V) + e + (tid & 15) * 8);
         }
+        return p;
     };
-    auto store_tile = [&](int kt) {
-        u32x4 *kb = tiles + (kt & 1) * 2 * kPieces, *vb = kb + kPieces;
+    auto load_tile = [&](const T *base, int kt, int buffer, int of) {
+        const bool full = (kt + 1) * kKeys <= nk;
+        const uint32_t at = lds0 + buffer * kTileBytes;
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const int r = i * (kWG / 16) + tid / 16;
-            // (weight 0 times whatever lies behind the last key must be 0)
-            if (kt * kKeys + r >= nk) vr[i] = (u32x4)(0u);
-            kb[k_piece(r, tid & 15)] = kr[i];
-            vb[v_piece(r, tid & 15)] = vr[i];
+        for (int i = 0; i < kKeys / 16; ++i) {
+            const int t0 = kt * kKeys + i * 16;
+            const T *src = base;
+            if constexpr (PAGED) {
+                const int64_t p = __builtin_amdgcn_readlane(of, i);
+                src += (((p * a.Hkv + kvh) << a.page_log2) + (min(t0, nk - 1) & ((1 << a.page_log2) - 1) & ~15)) * kD;
+                if (full) load_to_lds(src, at + i * 4096);
+                else load_to_lds(src + (min(t0 + lane_row, nk - 1) - (min(t0, nk - 1) & ~15) - lane_row) * kD, at + i * 4096);
+            } else {
+                src += t0 * a.kv_stride;
+                if (full) load_to_lds(src, at + i * 4096);
+                else load_to_lds(src + (int64_t)min(0, nk - 1 - t0 - lane_row) * a.kv_stride, at + i * 4096);
+            }
         }
     };
 
-    if (n_kt > 0) {
-        load_tile(0);
-        store_tile(0);
-    }
-    __syncthreads();
-    for (int kt = 0; kt < n_kt; ++kt) {
-        const bool more = kt + 1 < n_kt;
-        if (more) load_tile(kt + 1);
-        if (kt * kKeys <= wave_last) {
-            const u32x4 *kb = tiles + (kt & 1) * 2 * kPieces, *vb = kb + kPieces;
-            f32x16 S[2];
+    auto scores = [&](int buffer, f32x16 (&S)[2]) {
+        const u32x4 *kb = tiles + buffer * kPieces;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                S[b] = (f32x16)(0.0f);
+        for (int b = 0; b < 2; ++b) S[b] = (f32x16)(0.0f);
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const vec8 k = __builtin_bit_cast(vec8, kb[k_piece(b * 32 + lo, 2 * x + hi)]);
-                    S[b] = Mma<T>::dot(k, q[x], S[b]);
-                }
-            }
-            // (only the tiles that hold the last keys of some row of the wavefront)
-            if (kt * kKeys + kKeys - 1 > min(wave_first, nk - 1)) {
-                const int left = min(my_last, nk - 1) - kt * kKeys - 4 * hi;
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (b * 32 + 8 * (i / 4) + i % 4 > left) S[b][i] = kNegInf;
-            }
-            float top = kNegInf;
+        for (int x = 0; x < 8; ++x)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
+                S[b] = Mma<T>::dot(__builtin_bit_cast(vec8, kb[k_piece(b * 32 + lo, 2 * x + hi)]), q[x], S[b]);
+    };
+    auto hide = [&](int kt, f32x16 (&S)[2]) {
+        const int left = my_last - kt * kKeys - 4 * hi;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, S[b][i]);
-            top = halves_max(top) * kPromptScale;
-            if (__any(top > m + kSlack)) {
-                const float mn = fmaxf(m, top);
-                const float f = __builtin_amdgcn_exp2f(m - mn);
-                m = mn;
-                l *= f;
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int d = 0; d < 4; ++d) O[d] *= f;
+            for (int i = 0; i < 16; ++i)
+                if (b * 32 + 8 * (i / 4) + i % 4 > left) S[b][i] = kNegInf;
+    };
+    auto weights = [&](const f32x16 (&S)[2], vec8 (&P)[4], int c0 = 0, int c1 = 4) {
+        const float shift = kRoom - m;
+#pragma unroll
+        for (int c = c0; c < c1; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                P[c][j] = (T)__builtin_amdgcn_exp2f(__builtin_fmaf(S[c / 2][8 * (c & 1) + j], kPromptScale, shift));  // (rounded once, to the type of V)
+    };
+    auto add_up = [&](const vec8 (&P)[4]) {   // (the rounded weights)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) l = Mma<T>::add2((typename Mma<T>::vec2){P[c][j], P[c][j + 1]}, l);
+    };
+    auto values = [&](int buffer, const vec8 (&P)[4], int c0 = 0, int c1 = 4) {
+        const u32x4 *vb = tiles + (2 + buffer) * kPieces;
+#pragma unroll
+        for (int c = c0; c < c1; ++c)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                // four keys by sixteen channels for each 16 lanes: lane 4 j + x brings row j, channels 4 x ..
+                const int r = 16 * c + 4 * hi + (lane & 15) / 4, piece = d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2;
+                const char *v0 = reinterpret_cast<const char *>(vb + v_piece(r, piece)) + (lane & 1) * 8;
+                const char *v1 = reinterpret_cast<const char *>(vb + v_piece(r + 8, piece)) + (lane & 1) * 8;
+                const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v0);
+                const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v1);
+                const s16x8 v = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+                O[d] = Mma<T>::dot(__builtin_bit_cast(vec8, v), P[c], O[d]);
             }
-            const float shift = kRoom - m;
-            vec8 P[4];
+    };
+    auto raise = [&](const f32x16 (&S)[2]) {
+        float top = kNegInf;
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[c / 2][8 * (c & 1) + j], kPromptScale, shift));
-                    l += p;
-                    P[c][j] = (T)p;  // (rounded once to the type of V; the sum is that of the weights before it)
-                }
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, S[b][i]);
+        top = halves_max(top) * kPromptScale;
+        if (__any(top > m + kSlack)) {
+            const float mn = fmaxf(m, top);
+            const float f = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= f;
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    // four keys by sixteen channels for each 16 lanes: lane 4 j + x brings row j, channels 4 x ..
-                    const int r = 16 * c + 4 * hi + (lane & 15) / 4, piece = d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2;
-                    const char *v0 = reinterpret_cast<const char *>(vb + v_piece(r, piece)) + (lane & 1) * 8;
-                    const char *v1 = reinterpret_cast<const char *>(vb + v_piece(r + 8, piece)) + (lane & 1) * 8;
-                    const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v0);
-                    const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v1);
-                    const s16x8 v = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
-                    O[d] = Mma<T>::dot(__builtin_bit_cast(vec8, v), P[c], O[d]);
-                }
+            for (int d = 0; d < 4; ++d) O[d] *= f;
         }
-        if (more) store_tile(kt + 1);
-        __syncthreads();
+    };
+    // (the loads of q are waited for here: inside the loop the wait would take in the next tile's loads as well)
+#pragma unroll
+    for (int x = 0; x < 8; ++x) asm volatile("" : "+v"(q[x]));
+
+    int ids0 = page_ids(0), ids1 = page_ids(1);
+    if (n_kt > 0) {
+        load_tile(Kp, 0, 0, ids0);
+        load_tile(Vp, 0, 2, ids0);
+        if (n_kt > 1) load_tile(Kp, 1, 1, ids1);
+    }
+    ids0 = page_ids(2);
+    wait_tiles();
+    f32x16 S0[2], S1[2];
+    if (n_mine > 0) {
+        scores(0, S0);
+        if (n_clear < 1) hide(0, S0);
+        raise(S0);
+    }
+    // A step: most of tile kt's weights while the matrix units form the scores of the next, the rest while they form its
+    // values, with the sum of the weights and the next one's maximum (so that both halves have vector work, and registers do); the K tile after the next and the next V tile are on their way meanwhile, to
+    // places whose tiles were done with before the last barrier.  odd: kt % 2
+    auto bring = [&](int kt, int odd) {
+        if (kt + 1 < n_kt) load_tile(Vp, kt + 1, 3 - odd, ids1);
+        if (kt + 2 < n_kt) load_tile(Kp, kt + 2, odd, ids0);
+        ids1 = ids0;
+        ids0 = page_ids(kt + 3);
+    };
+    auto step = [&](int kt, int odd, f32x16 (&S)[2], f32x16 (&N)[2], auto hidden) {
+        bring(kt, odd);
+        vec8 P[4];
+        scores(1 - odd, N);
+        weights(S, P, 0, 3);
+        if (hidden) hide(kt + 1, N);
+        values(odd, P, 0, 3);
+        weights(S, P, 3, 4);
+        values(odd, P, 3, 4);
+        add_up(P);
+        raise(N);
+        wait_tiles();
+    };
+    int kt = 0;
+    for (; kt + 2 < n_clear; kt += 2) {
+        step(kt, 0, S0, S1, std::false_type{});
+        step(kt + 1, 1, S1, S0, std::false_type{});
+    }
+    for (; kt + 1 < n_mine; ++kt) {
+        step(kt, kt & 1, S0, S1, std::true_type{});
+        S0[0] = S1[0];
+        S0[1] = S1[1];
+    }
+    for (; kt < n_kt; ++kt) {   // (the wavefront's last tile, and those that only others see)
+        bring(kt, kt & 1);
+        if (kt < n_mine) {
+            vec8 P[4];
+            weights(S0, P);
+            values(kt & 1, P);
+            add_up(P);
+        }
+        wait_tiles();
     }
     if constexpr (PAGED) {  // (a page that is not there: seen by the threads that would have read it)
         uint32_t *flag = reinterpret_cast<uint32_t *>(tiles);
