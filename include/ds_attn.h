@@ -340,8 +340,8 @@ ds_status_t ds_attend_rows(const void *q, const void *KV_rows, float *out,
  * n_seqs < 1, total_q < 0, max_kv < 0, bad heads, d != 128, a stride below the row it steps over or
  * beyond 2^30 (kv_head_stride: 2^40), an unknown dtype, or (total_q / 128 + n_seqs) * Hq beyond 2^24 -> DS_ERR_SHAPE.  What is on the device is checked there: a
  * sequence whose new tokens do not lie in [0, total_q) is not computed (its rows are left as they are), one
- * whose keys do not lie within kv_elems, within its row of the page table or on pages of the pool
- * gets NaN, and nothing is read outside.
+ * whose keys do not lie within kv_elems, within its row of the page table or on pages of the pool, or are more than
+ * 2^30, gets NaN, and nothing is read outside.
  * max_kv: keys of the longest sequence (a guide to the split, which the results do not rest on).
  */
 typedef enum { DS_F16 = 0, DS_BF16 = 1 } ds_dtype_t; /* IEEE binary16; bfloat16 */
@@ -362,8 +362,8 @@ typedef struct {
  * is a row of the page table, table [n_rows, max_pages] int32: its token t lies in page
  * table[row, t / page_tokens], place t % page_tokens, for t < lens[row] (lens [n_rows] int32).  Entries past
  * the last page are not read.  All layers share table and lens.  Rows of a page past the last token may hold anything.
- * page_tokens: 16, 32, 64, 128 or 256.  1 <= n_pages <= 2^20, 1 <= n_rows <= 65536, max_pages * page_tokens < 2^31,
- * else DS_ERR_SHAPE.  Pools 256-byte aligned.
+ * page_tokens: 16, 32, 64, 128 or 256.  1 <= n_pages <= 2^20, 1 <= n_rows <= 65536, max_pages * page_tokens <=
+ * 2^30, else DS_ERR_SHAPE.  Pools 256-byte aligned.
  */
 typedef struct {
     int32_t n_pages, page_tokens, Hkv, d; /* pages of a pool, tokens of a page, KV heads, head dim (=128) */
@@ -390,7 +390,7 @@ ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const 
  * and the workspace are sized for, a guide that the results do not rest on, but bits of a sum may.  A sequence without a token gives
  * zeros; one whose row, length or pages cannot be gives NaN, and nothing is read outside the table and the pools.
  * Pools 256-byte aligned, q, out and workspace 16-byte.  n_seqs, Hq < 1, bad heads, rows NULL with n_seqs > n_rows,
- * or n_seqs * Hkv * ceil(G / 16) * ceil(max_pages * page_tokens / 64) beyond 2^31 -> DS_ERR_SHAPE.
+ * or n_seqs * Hkv * ceil(G / 16) * (ceil(max_pages * page_tokens / 64) + 3) beyond 2^31 -> DS_ERR_SHAPE.
  */
 size_t ds_paged_workspace_bytes(const ds_pages_t *pages, int32_t n_seqs, int32_t Hq, int32_t max_len);
 ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pages, float *out,

@@ -43,7 +43,7 @@ static bool pages_ok(const ds_pages_t *p)
 {
     if (p->page_tokens < 16 || p->page_tokens > 256 || (p->page_tokens & (p->page_tokens - 1))) return false;
     if (p->n_pages < 1 || p->n_pages > 1 << 20 || p->n_rows < 1 || p->n_rows > 65536 || p->max_pages < 1) return false;
-    return (int64_t)p->max_pages * p->page_tokens < 1ll << 31 && heads_ok(p->Hkv, p->Hkv, p->d, p->dtype);
+    return (int64_t)p->max_pages * p->page_tokens <= kMostTokens && heads_ok(p->Hkv, p->Hkv, p->d, p->dtype);
 }
 
 static int log2_of(int x) { return __builtin_ctz((unsigned)x); }
@@ -132,7 +132,7 @@ static bool paged_ok(const ds_pages_t *g, int32_t n_seqs, int32_t Hq, int32_t ma
 {
     if (!pages_ok(g) || n_seqs < 1 || max_len < 0 || !heads_ok(Hq, g->Hkv, g->d, g->dtype)) return false;
     const int64_t units = (int64_t)n_seqs * g->Hkv * ((Hq / g->Hkv + 15) / 16);
-    return units <= (1ll << 31) / (((int64_t)g->max_pages * g->page_tokens + kPiece - 1) / kPiece);
+    return units <= (1ll << 31) / (((int64_t)g->max_pages * g->page_tokens + kPiece - 1) / kPiece + kLead);
 }
 
 size_t ds_paged_workspace_bytes(const ds_pages_t *pages, int32_t n_seqs, int32_t Hq, int32_t max_len)
@@ -171,6 +171,7 @@ ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pa
     a.G = p.G;
     a.passes = p.passes;
     a.least = p.least;
+    a.join_here = p.join_here;
     a.n_pages = pages->n_pages;
     a.page_log2 = log2_of(pages->page_tokens);
     a.max_pages = pages->max_pages;

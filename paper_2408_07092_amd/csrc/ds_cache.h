@@ -17,6 +17,8 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kMostTokens = 1 << 30;  // of a sequence: what the kernels step past its end stays within 32 bits
+
 // ---------------------------------------------------------------- prompt attention
 constexpr int kPromptRows = 128;   // rows (token * G + head of the group) of a workgroup
 
@@ -59,6 +61,7 @@ __device__ __forceinline__ int last_at_or_before(int n, int x, Key key)
 
 // ---------------------------------------------------------------- paged decode
 constexpr int kPiece = 64;         // tokens that a share is counted in: 16 for each wavefront of a workgroup
+constexpr int kLead = 3;           // pieces that a unit counts for besides its own
 
 struct PagedArgs {
     const void *q, *K, *V;
@@ -66,10 +69,12 @@ struct PagedArgs {
     uint32_t *arrived;             // per sequence and unit, zero between calls
     const int32_t *rows, *lens, *table;
     int n, Hkv, G, passes, least;  // passes of 16 heads over a KV head's rows; least pieces of a share
+    bool join_here;                // parts are joined by the workgroup that is last, not by a launch after this one
     int n_pages, page_log2, max_pages, n_table;
 };
 struct PagedPlan {
     int G, passes, GH, least, wgs;
+    bool join_here;
     size_t off_part, total;
 };
 void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan *p);

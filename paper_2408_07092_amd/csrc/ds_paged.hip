@@ -9,6 +9,13 @@
 // the last workgroup to arrive joins them in their order along the cache.  Which part holds
 // which tokens follows from the lengths and the launch alone, so results do not depend on who is last.
 //
+// One workgroup to a compute unit, each wavefront with two tiles of 16 tokens on their way (64 KiB a compute unit), streams best: 16
+// sequences of 32K tokens (2.1 GB) take 322 us, 6.6 TB/s; with one tile on its way and one, two or four
+// workgroups 405, 318 and 347; with two tiles and two workgroups 332; one sequence of 250K (512 MB) 89, and 118 to
+// 182 with one tile and two to four workgroups, whose parts cost more to join.  A unit's beginning and end (its query, the
+// wavefronts' states, the part) cost a workgroup about what three pieces do, and count as kLead pieces: 48 sequences of 3 to 20000
+// tokens 157 us without, 109, 102 and 100 with one, two and three.
+//
 // A wavefront takes 16 tokens at a time (within one page, as pages hold 16 or more), for up to 16 heads
 // of the group at once:
 //   S[token][head] = K[token][:] . q[head][:]       16x16x32, K and q from memory
@@ -53,7 +60,8 @@ __device__ __forceinline__ int row_tokens(const PagedArgs &a, int b, int *row)
     const int n = a.lens[*row];
     return n < 0 || (int64_t)n > (int64_t)a.max_pages << a.page_log2 ? -1 : n;
 }
-__device__ __forceinline__ int pieces_of(int tokens) { return tokens > 0 ? (tokens - 1) / kPiece + 1 : 0; }
+// ... and what they count for: the pieces, and kLead more for a unit's beginning and end.
+__device__ __forceinline__ int pieces_of(int tokens) { return tokens > 0 ? (tokens - 1) / kPiece + 1 + kLead : 0; }
 
 // The share of workgroup w of W: T / W pieces, the first T % W of them one more.
 struct Shares {
@@ -68,12 +76,12 @@ struct Shares {
 
 // Joins the parts of a unit, which lie with workgroups w0 .. w1: for every head
 //   y = sum_p acc_p 2^(m_p - M) / sum_p l_p 2^(m_p - M),  M = max_p m_p,
-// a wavefront for a head, or two or four of them where there are fewer heads, 12 or 16 parts in flight (as registers allow), folded in
+// a wavefront for a head, or two or four of them where there are fewer heads, 16 parts in flight, folded in
 // an order that depends on the launch alone.  All threads call it.
 template <int GH>
-__device__ __forceinline__ void join_parts(const PagedArgs &a, int w0, int w1, int n_heads, float *out, float (*red)[kD + 4])
+__device__ __forceinline__ void join_parts(const PagedArgs &a, int w0, int w1, int first_head, int n_heads, float *out, float (*red)[kD + 4])
 {
-    constexpr int kBatch = 12;
+    constexpr int kBatch = 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int share = n_heads >= 4 ? 1 : n_heads >= 2 ? 2 : 4, at_once = 4 / share;
     const int n = w1 - w0 + 1, sub = wave % share;
@@ -87,7 +95,7 @@ __device__ __forceinline__ void join_parts(const PagedArgs &a, int w0, int w1, i
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
                     const int w = w0 + min(i0 + i * share, n - 1);
-                    const float *pc = a.part + (((size_t)w * 2 + (w == w0 ? 1 : 0)) * GH + g) * kPartStride;
+                    const float *pc = a.part + (((size_t)w * 2 + (w == w0 ? 1 : 0)) * GH + first_head + g) * kPartStride;
                     ml[i] = ld_dev(reinterpret_cast<const float2 *>(pc));
                     v[i] = ld_dev(reinterpret_cast<const float2 *>(pc + 4 + 2 * lane));
                 }
@@ -138,14 +146,30 @@ __device__ __forceinline__ void join_parts(const PagedArgs &a, int w0, int w1, i
     }
 }
 
-template <class T, int GH>
-__global__ __launch_bounds__(kWG, GH > 8 ? 3 : 4) void k_paged(PagedArgs a)
+// All pieces of the call's sequences, and those ahead of sequence `upto` (threads of a workgroup each take some).
+__device__ __forceinline__ void count_pieces(const PagedArgs &a, int upto, uint32_t *s_w, uint32_t *total, uint32_t *before)
 {
+    uint32_t all = 0, ahead = 0;
+    for (int b = threadIdx.x; b < a.n; b += kWG) {
+        int row;
+        const uint32_t k = (uint32_t)pieces_of(row_tokens(a, b, &row));
+        all += k;
+        if (b < upto) ahead += k;
+    }
+    block_exclusive_scan(all, s_w, total);
+    block_exclusive_scan(ahead, s_w, before);
+}
+__device__ __forceinline__ uint32_t shares_of(const PagedArgs &a, uint32_t T_all, uint32_t wgs) { return max(1u, min(wgs, T_all / (uint32_t)a.least)); }
+
+template <class T, int GH>
+__global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
+{
+    constexpr int kDepth = 2;   // tiles of a wavefront on their way
     typedef typename Mma16<T>::vec8 vec8;
     typedef typename Mma16<T>::vec4 vec4;
     __shared__ __attribute__((aligned(16))) float wpart[4][GH][kPartStride];
     __shared__ __attribute__((aligned(16))) float sc_sh[4][16];
-    __shared__ uint32_t s_w[4], s_flag, s_at[2];
+    __shared__ uint32_t s_w[4], s_flag, s_at[4];
     float (*red)[kD + 4] = reinterpret_cast<float (*)[kD + 4]>(&wpart[0][0][0]);   // (4 of them; used after wpart)
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 15, hi = lane >> 4;
@@ -153,9 +177,10 @@ __global__ __launch_bounds__(kWG, GH > 8 ? 3 : 4) void k_paged(PagedArgs a)
     // ---- all pieces, and where this workgroup's share starts
     const int per = (a.n + kWG - 1) / kWG;
     uint32_t mine = 0;
+    int n = 1, row = 0;
     for (int i = 0; i < per; ++i) {
         const int b = tid * per + i;
-        int row, n = 1;
+        n = 1;
         if (b < a.n) {
             n = row_tokens(a, b, &row);
             mine += (uint32_t)pieces_of(n);
@@ -171,37 +196,42 @@ __global__ __launch_bounds__(kWG, GH > 8 ? 3 : 4) void k_paged(PagedArgs a)
     uint32_t total;
     uint32_t ahead = block_exclusive_scan(mine, s_w, &total);
     const uint32_t T_all = total * (uint32_t)units;
-    const uint32_t W = max(1u, min(gridDim.x, T_all / (uint32_t)a.least));
+    const uint32_t W = shares_of(a, T_all, gridDim.x);
     if (blockIdx.x >= W || T_all == 0) return;
     const Shares shares(T_all, W);
     uint32_t x = shares.start(blockIdx.x);
     const uint32_t x_end = shares.start(blockIdx.x + 1);
     const uint32_t want = x / (uint32_t)units;     // the piece of a sequence that the share starts in, counted over sequences
     if (ahead <= want && want < ahead + mine) {
-        int b = tid * per, row;
-        for (uint32_t k; (k = (uint32_t)pieces_of(row_tokens(a, b, &row))) <= want - ahead; ++b) ahead += k;
+        int b = tid * per;
+        if (per > 1)
+            for (uint32_t k; (k = (uint32_t)pieces_of(n = row_tokens(a, b, &row))) <= want - ahead; ++b) ahead += k;
         s_at[0] = (uint32_t)b;
         s_at[1] = ahead;
+        s_at[2] = (uint32_t)n;
+        s_at[3] = (uint32_t)row;
     }
     __syncthreads();
     int b = __builtin_amdgcn_readfirstlane((int)s_at[0]);
     uint32_t seq0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_at[1]) * (uint32_t)units;       // first piece of sequence b
+    n = __builtin_amdgcn_readfirstlane((int)s_at[2]);
+    row = __builtin_amdgcn_readfirstlane((int)s_at[3]);
 
     while (x < x_end) {
-        int row;
-        const int n = row_tokens(a, b, &row);
         const uint32_t np = (uint32_t)pieces_of(n);
-        if (x >= seq0 + np * (uint32_t)units) {    // (also over sequences without a piece)
+        if (x >= seq0 + np * (uint32_t)units) {    // on to the next sequence (also over those without a piece)
             seq0 += np * (uint32_t)units;
-            ++b;
+            n = row_tokens(a, ++b, &row);
             continue;
         }
         const int u = (int)((x - seq0) / np), h = u / a.passes, g0 = (u % a.passes) * 16;
         const uint32_t unit0 = seq0 + (uint32_t)u * np;
-        const int p0 = (int)(x - unit0), p1 = (int)min(np, x_end - unit0);
+        // (a share that ends within a unit's lead leaves it to the next)
+        const int p0 = max((int)(x - unit0) - kLead, 0), p1 = (int)min(np, x_end - unit0) - kLead;
         const int n_heads = min(16, a.G - g0);
         const size_t head0 = (size_t)b * a.Hkv * a.G + (size_t)h * a.G + g0;
-        x = unit0 + p1;
+        x = unit0 + kLead + p1;
+        if (p1 <= 0) break;
 
         // ---- the wavefront's tiles: tokens 64 p + 16 wave ..
         vec8 q[4];
@@ -215,8 +245,11 @@ __global__ __launch_bounds__(kWG, GH > 8 ? 3 : 4) void k_paged(PagedArgs a)
 #pragma unroll
         for (int e = 0; e < 8; ++e) O[e] = (f32x4)(0.0f);
         bool bad = false;
-        const int32_t *pages = a.table + (size_t)row * a.max_pages;
-        vec8 kr[4], vr[4];
+        // (read as constants: by scalar loads, which do not queue behind the rows)
+        const auto *pages = (const __attribute__((address_space(4))) int32_t *)(a.table + (size_t)row * a.max_pages);
+        int t = p0 * kPiece + wave * 16;
+        const int t_end = min(n, p1 * kPiece);
+        const int t_last = t + (t_end - 1 - t) / kPiece * kPiece;   // the wavefront's last tile, if it has one
         auto place = [&](int p, int t) {   // element of the pools where the tile that starts with token t starts, in page p
             if ((uint32_t)p >= (uint32_t)a.n_pages) {
                 bad = true;
@@ -224,79 +257,98 @@ __global__ __launch_bounds__(kWG, GH > 8 ? 3 : 4) void k_paged(PagedArgs a)
             }
             return ((((int64_t)p * a.Hkv + h) << a.page_log2) + (t & ((1 << a.page_log2) - 1))) * kD;
         };
-        auto issue_k = [&](int64_t at) {
+        auto page_of = [&](int t) { return pages[min(t, t_last) >> a.page_log2]; };
+        struct Rows {
+            vec8 k[4], v[4];
+        };
+        auto issue_k = [&](Rows &rows, int64_t at) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                kr[i] = __builtin_nontemporal_load(reinterpret_cast<const vec8 *>(static_cast<const T *>(a.K) + at + lo * kD + 8 * (4 * i + hi)));
+                rows.k[i] = __builtin_nontemporal_load(reinterpret_cast<const vec8 *>(static_cast<const T *>(a.K) + at + lo * kD + 8 * (4 * i + hi)));
         };
-        auto issue_v = [&](int64_t at) {
+        auto issue_v = [&](Rows &rows, int64_t at) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                vr[r] = __builtin_nontemporal_load(reinterpret_cast<const vec8 *>(static_cast<const T *>(a.V) + at + (4 * hi + r) * kD + 8 * lo));
+                rows.v[r] = __builtin_nontemporal_load(reinterpret_cast<const vec8 *>(static_cast<const T *>(a.V) + at + (4 * hi + r) * kD + 8 * lo));
         };
-        int t = p0 * kPiece + wave * 16;
-        const int t_end = min(n, p1 * kPiece);
-        if (t < t_end) {
-            // (a tile's page is looked up while the tile before the one before it is computed)
-            const int last_entry = (n - 1) >> a.page_log2;
-            int64_t at = place(pages[t >> a.page_log2], t);
-            int page = pages[min((t + kPiece) >> a.page_log2, last_entry)];
-            issue_k(at);
-            issue_v(at);
-            for (; t < t_end; t += kPiece) {
-                const bool more = t + kPiece < t_end;
-                if (more) at = place(page, t + kPiece);
-                page = pages[min((t + 2 * kPiece) >> a.page_log2, last_entry)];
-                __builtin_amdgcn_sched_barrier(0);
-                f32x4 S = (f32x4)(0.0f);
+        // Folds the tile that starts with token t into the state; its rows' registers are loaded again, for the tile
+        // kDepth ahead, as soon as they are used up: a wavefront has 16 KiB on their way.
+        auto fold = [&](Rows &rows, int t, auto more, int64_t at) {
+            __builtin_amdgcn_sched_barrier(0);
+            f32x4 S = (f32x4)(0.0f);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) S = Mma16<T>::dot32(kr[i], q[i], S);
-                __builtin_amdgcn_sched_barrier(0);
-                if (more) issue_k(at);
-                __builtin_amdgcn_sched_barrier(0);
-                float s[4];
+            for (int i = 0; i < 4; ++i) S = Mma16<T>::dot32(rows.k[i], q[i], S);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more()) issue_k(rows, at);
+            __builtin_amdgcn_sched_barrier(0);
+            float s[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[r] = t + 4 * hi + r < n ? S[r] * kScaleLog2 : kNegInf;
-                if (t + 16 > n) {   // (rows of the page behind the last token: weight 0 times whatever is there must be 0)
+            for (int r = 0; r < 4; ++r) s[r] = t + 4 * hi + r < n ? S[r] * kScaleLog2 : kNegInf;
+            if (t + 16 > n) {   // (rows of the page behind the last token: weight 0 times whatever is there must be 0)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (t + 4 * hi + r >= n) vr[r] = (vec8)(T)0;
-                }
-                const float mn = fmaxf(m, rows_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));  // (token t is there)
-                const float sc = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
-                m = mn;
-                float p[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - mn + kPScaleLog2);
-                l = l * sc + ((p[0] + p[1]) + (p[2] + p[3]));
-                if (__any(sc != 1.0f)) {
-                    if (hi == 0) sc_sh[wave][lo] = sc;
-                    const f32x4 f = *reinterpret_cast<const f32x4 *>(&sc_sh[wave][4 * hi]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) O[e] *= f;
-                }
-                // a weight as the sum of two numbers of V's type: 22 bits in fp16 (the scale keeps the low part normal), 16 in bf16
-                vec4 p_hi, p_lo;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    p_hi[r] = (T)p[r];
-                    p_lo[r] = (T)(p[r] - (float)p_hi[r]);
-                }
-                // (four high parts, then the four low parts: two issues in a row into one accumulator would wait for each other)
-#pragma unroll
-                for (int e0 = 0; e0 < 8; e0 += 4) {
-                    vec4 v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = (vec4){vr[0][e0 + e], vr[1][e0 + e], vr[2][e0 + e], vr[3][e0 + e]};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) O[e0 + e] = Mma16<T>::dot16(p_hi, v[e], O[e0 + e]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) O[e0 + e] = Mma16<T>::dot16(p_lo, v[e], O[e0 + e]);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                if (more) issue_v(at);
+                for (int r = 0; r < 4; ++r)
+                    if (t + 4 * hi + r >= n) rows.v[r] = (vec8)(T)0;
             }
+            const float mn = fmaxf(m, rows_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));  // (token t is there)
+            const float sc = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            float p[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - mn + kPScaleLog2);
+            l = l * sc + ((p[0] + p[1]) + (p[2] + p[3]));
+            if (__any(sc != 1.0f)) {
+                if (hi == 0) sc_sh[wave][lo] = sc;
+                const f32x4 f = *reinterpret_cast<const f32x4 *>(&sc_sh[wave][4 * hi]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) O[e] *= f;
+            }
+            // a weight as the sum of two numbers of V's type: 22 bits in fp16 (the scale keeps the low part normal), 16 in bf16
+            vec4 p_hi, p_lo;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p_hi[r] = (T)p[r];
+                p_lo[r] = (T)(p[r] - (float)p_hi[r]);
+            }
+            // (four high parts, then the four low parts: two issues in a row into one accumulator would wait for each other)
+#pragma unroll
+            for (int e0 = 0; e0 < 8; e0 += 4) {
+                vec4 v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = (vec4){rows.v[0][e0 + e], rows.v[1][e0 + e], rows.v[2][e0 + e], rows.v[3][e0 + e]};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[e0 + e] = Mma16<T>::dot16(p_hi, v[e], O[e0 + e]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[e0 + e] = Mma16<T>::dot16(p_lo, v[e], O[e0 + e]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more()) issue_v(rows, at);
+        };
+        if (t < t_end) {
+            Rows rows[kDepth];
+            int page[kDepth];
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) page[d] = page_of(t + d * kPiece);
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                const int64_t at = place(page[d], min(t + d * kPiece, t_last));
+                issue_k(rows[d], at);
+                issue_v(rows[d], at);
+            }
+            // (pages are looked up while the tiles before are computed; past its last tile a wavefront reads that
+            //  one again, in the caches, so that no load is a choice and every wait is for the loads that it needs)
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) page[d] = page_of(t + (kDepth + d) * kPiece);
+            for (; t + (kDepth - 1) * kPiece < t_end; t += kDepth * kPiece) {
+#pragma unroll
+                for (int d = 0; d < kDepth; ++d) {
+                    const int64_t at = place(page[d], min(t + (kDepth + d) * kPiece, t_last));
+                    page[d] = page_of(t + (2 * kDepth + d) * kPiece);
+                    fold(rows[d], t + d * kPiece, std::true_type{}, at);
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < kDepth - 1; ++d)
+                if (t + d * kPiece < t_end) fold(rows[d], t + d * kPiece, std::false_type{}, 0);
         }
         // ---- the wavefronts' states as one part, or the result
         l = rows_sum(l);
@@ -314,20 +366,40 @@ __global__ __launch_bounds__(kWG, GH > 8 ? 3 : 4) void k_paged(PagedArgs a)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) wpart[wave][4 * hi + rr][4 + 8 * lo + e] = O[e][rr];
             }
-        const bool whole = p0 == 0 && p1 == (int)np;
+        const bool whole = p0 == 0 && p1 == (int)np - kLead;
         // (a share has at most one part of a unit that an earlier share began, and one of a unit that goes on)
         float *po = a.part + ((size_t)blockIdx.x * 2 + (p0 == 0 ? 1 : 0)) * GH * kPartStride;
         wg_combine_store<GH>(wpart, n_heads, po, kPartStride, whole ? a.out + head0 * kD : nullptr);
-        if (!whole) {
-            const int w0 = (int)shares.of(unit0), w1 = (int)shares.of(unit0 + np - 1);
+        if (!whole && a.join_here) {
+            const int w0 = (int)shares.of(unit0 + kLead), w1 = (int)shares.of(unit0 + np - 1);
             uint32_t *arrived = a.arrived + (size_t)b * units + u;
             if (last_arrival(arrived, (uint32_t)(w1 - w0 + 1), &s_flag)) {
                 if (tid == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                join_parts<GH>(a, w0, w1, n_heads, a.out + head0 * kD, red);
+                join_parts<GH>(a, w0, w1, 0, n_heads, a.out + head0 * kD, red);
             }
         }
         __syncthreads();   // (wpart is written again)
     }
+}
+
+// The join as a launch of its own, a workgroup for every query head: where few units are cut into many parts, one
+// workgroup at the end of the launch above would read a unit's parts for all of its heads.
+template <int GH>
+__global__ __launch_bounds__(kWG) void k_paged_join(PagedArgs a, uint32_t wgs)
+{
+    __shared__ __attribute__((aligned(16))) float red[4][kD + 4];
+    __shared__ uint32_t s_w[4];
+    const int Hq = a.Hkv * a.G, b = blockIdx.x / Hq, hq = blockIdx.x % Hq, units = a.Hkv * a.passes;
+    uint32_t total, ahead;
+    count_pieces(a, b, s_w, &total, &ahead);
+    int row;
+    const uint32_t np = (uint32_t)pieces_of(row_tokens(a, b, &row)), T_all = total * (uint32_t)units;
+    if (np == 0) return;
+    const Shares shares(T_all, shares_of(a, T_all, wgs));
+    const int h = hq / a.G, g = hq % a.G;
+    const uint32_t unit0 = ahead * (uint32_t)units + (uint32_t)(h * a.passes + g / 16) * np;
+    const int w0 = (int)shares.of(unit0 + kLead), w1 = (int)shares.of(unit0 + np - 1);
+    if (w0 != w1) join_parts<GH>(a, w0, w1, g % 16, 1, a.out + (size_t)blockIdx.x * kD, red);
 }
 
 // Writes new tokens' rows into their pages: a wavefront takes a token and 16 of its 2 Hkv rows, four
@@ -367,21 +439,28 @@ void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan 
     p->G = Hq / g.Hkv;
     p->passes = (p->G + 15) / 16;
     p->GH = p->G <= 4 ? 4 : p->G <= 8 ? 8 : 16;
+    // Shares of no less than two pieces (one sequence of 900 tokens, 32 heads: 10.8 us, of four 11.7, of eight 14.0).
     p->least = 2;
-    const int64_t pieces = (int64_t)n * g.Hkv * p->passes * std::max(1, (max_len + kPiece - 1) / kPiece);
-    p->wgs = (int)std::min<int64_t>(pieces, device_caps().cus * (p->GH > 8 ? 3 : 4));
-    p->off_part = ((size_t)n * g.Hkv * p->passes * 4 + 255) / 256 * 256;
+    const int64_t units = (int64_t)n * g.Hkv * p->passes, pieces = units * std::max(1, (max_len + kPiece - 1) / kPiece);
+    p->wgs = (int)std::min<int64_t>(pieces, device_caps().cus);
+    // Up to eight parts a unit the last workgroup joins for all heads (32 units of 900 tokens 10.8 us, with a launch of its own
+    // for the join 11.9); more are joined by a workgroup for each head (4 units of 250K tokens, 64 parts: 119 -> 110).
+    p->join_here = p->wgs <= 8 * units;
+    p->off_part = ((size_t)units * 4 + 255) / 256 * 256;
     p->total = (p->off_part + (size_t)p->wgs * 2 * p->GH * kPartStride * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_paged(PagedArgs a, const PagedPlan &p, int dtype, hipStream_t st)
 {
-    const dim3 grid((unsigned)p.wgs);
     const bool bf = dtype == DS_BF16;
     void (*fn)(PagedArgs) = p.GH == 4   ? (bf ? k_paged<__bf16, 4> : k_paged<_Float16, 4>)
                             : p.GH == 8 ? (bf ? k_paged<__bf16, 8> : k_paged<_Float16, 8>)
                                         : (bf ? k_paged<__bf16, 16> : k_paged<_Float16, 16>);
-    DS_LAUNCH(KID_PAGED, fn, grid, dim3(kWG), 0, st, a);
+    DS_LAUNCH(KID_PAGED, fn, dim3((unsigned)p.wgs), dim3(kWG), 0, st, a);
+    if (!p.join_here) {
+        void (*join)(PagedArgs, uint32_t) = p.GH == 4 ? k_paged_join<4> : p.GH == 8 ? k_paged_join<8> : k_paged_join<16>;
+        DS_LAUNCH(KID_PAGED, join, dim3((unsigned)(a.n * a.Hkv * a.G)), dim3(kWG), 0, st, a, (uint32_t)p.wgs);
+    }
     return hipGetLastError();
 }
 

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     } else {
         nk = a.kv_len[s];
         kv0 = a.kv_start[s];
-        bad = nk < 0 || kv0 < 0 || (nk > 0 && (kv0 + nk - 1) * a.kv_stride + (int64_t)(a.Hkv - 1) * a.kv_head_stride + kD > a.kv_elems);
+        bad = nk < 0 || nk > kMostTokens || kv0 < 0 || (nk > 0 && (kv0 + nk - 1) * a.kv_stride + (int64_t)(a.Hkv - 1) * a.kv_head_stride + kD > a.kv_elems);
         kv0 = kv0 * a.kv_stride + (int64_t)kvh * a.kv_head_stride;
     }
     if (bad) nk = 0;
