@@ -406,10 +406,16 @@ __global__ __launch_bounds__(kWG) void k_paged_join(PagedArgs a, uint32_t wgs)
 // rows to an instruction, 16 lanes each.  Bound by memory: every row read once, written once.
 __global__ __launch_bounds__(kWG) void k_append_paged(AppendPagedArgs a)
 {
-    const int wave = (int)(blockIdx.x * (kWG / 64) + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (kWG / 64) + (threadIdx.x >> 6))), lane = threadIdx.x & 63;
     const int parts = (2 * a.Hkv + 15) / 16;
     const int i = wave / parts, x0 = (wave % parts) * 16;
     if (i >= a.total_new) return;
+    u32x4 v[4];   // (on their way while their place is looked up)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int x = x0 + 4 * e + (lane >> 4), h = x >> 1;
+        if (h < a.Hkv) v[e] = (x & 1 ? a.v_new : a.k_new)[(size_t)i * a.new_stride + (size_t)h * 16 + (lane & 15)];
+    }
     const int s = last_at_or_before(a.n, i, [&](int j) { return a.new_start[j]; });
     if (i < a.new_start[s] || i >= a.new_start[s + 1]) return;   // a row of no sequence
     const int row = a.rows ? a.rows[s] : s;
@@ -420,12 +426,6 @@ __global__ __launch_bounds__(kWG) void k_append_paged(AppendPagedArgs a)
     const int p = a.table[(size_t)row * a.max_pages + (t >> a.page_log2)];
     if ((uint32_t)p >= (uint32_t)a.n_pages) return;
     const int in_page = (int)(t & ((1 << a.page_log2) - 1));
-    u32x4 v[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int x = x0 + 4 * e + (lane >> 4), h = x >> 1;
-        if (h < a.Hkv) v[e] = (x & 1 ? a.v_new : a.k_new)[(size_t)i * a.new_stride + (size_t)h * 16 + (lane & 15)];
-    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int x = x0 + 4 * e + (lane >> 4), h = x >> 1;

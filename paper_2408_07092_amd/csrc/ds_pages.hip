@@ -33,29 +33,40 @@ __device__ __forceinline__ bool mark(const PagesArgs &a, uint32_t *seen, int r)
     return (atomicOr(&seen[r >> 5], bit) & bit) != 0u;
 }
 
+// The counts of 16 pages (pages that are none count as held), and which of them are free (bit i: the i-th).
+struct Counts {
+    typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+    i32x4 v[4];
+    __device__ __forceinline__ Counts(const int32_t *refs, int n_pages, int mine)
+    {
+        if (mine + 16 <= n_pages) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const i32x4 *>(refs + mine + 4 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i / 4][i % 4] = mine + i < n_pages ? refs[mine + i] : 1;
+        }
+    }
+    __device__ __forceinline__ uint32_t free() const
+    {
+        uint32_t f = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f |= v[i / 4][i % 4] <= 0 ? 1u << i : 0u;
+        return f;
+    }
+};
+
 // Goes through the free pages in ascending order, take(rank, page) for each, until `want` have been seen; how many
-// there are, or want if there are as many.  All threads of the workgroup call it.  take may write the
-// count of the page that it is given: a thread reads its 16 counts before it.
+// there are, or want if there are as many.  All threads of the workgroup call it.  first: the counts of the thread's
+// pages of the first round, which a caller can have asked for before.  take may write the count of the page that it is given (in
+// the first round it is read no more, in the others a thread has read its 16 before).
 template <class Take>
-__device__ __forceinline__ uint32_t each_free(const int32_t *refs, int n_pages, uint32_t want, uint32_t *s_w, Take take)
+__device__ __forceinline__ uint32_t each_free(const int32_t *refs, int n_pages, uint32_t want, uint32_t *s_w, const Counts &first, Take take)
 {
     uint32_t have = 0;
     for (int p0 = 0; p0 < n_pages && have < want; p0 += kBooks * 16) {
         const int mine = p0 + (int)threadIdx.x * 16;
-        uint32_t free = 0;
-        if (mine + 16 <= n_pages) {
-            typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-            i32x4 v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const i32x4 *>(refs + mine + 4 * i);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) free |= v[i][j] <= 0 ? 1u << (4 * i + j) : 0u;
-        } else {
-            for (int i = 0; i < 16 && mine + i < n_pages; ++i) free |= refs[mine + i] <= 0 ? 1u << i : 0u;
-        }
-        uint32_t total;
+        uint32_t free = p0 == 0 ? first.free() : Counts(refs, n_pages, mine).free(), total;
         uint32_t rank = have + block_exclusive_scan<kBookWaves>((uint32_t)__builtin_popcount(free), s_w, &total);
         for (; free && rank < want; free &= free - 1u, ++rank) take(rank, mine + __builtin_ctz(free));
         have += total;
@@ -70,6 +81,7 @@ __global__ __launch_bounds__(kBooks) void k_pages_extend(PagesArgs a)
     __shared__ uint32_t first[kPagesListed];   // pages that the list's entries before this one need
     __shared__ int32_t found[kFound];
     const int tid = threadIdx.x;
+    const Counts counts0(a.refs, a.n_pages, tid * 16);   // (asked for first: what they wait for is not needed before)
     for (int i = tid; i < 65536 / 32; i += kBooks) s.seen[i] = 0u;
     if (tid == 0) s.bad = 0u;
     __syncthreads();
@@ -117,7 +129,7 @@ __global__ __launch_bounds__(kBooks) void k_pages_extend(PagesArgs a)
         if (total > (uint32_t)a.n_pages) {
             code = DS_PAGES_NO_ROOM;
         } else {
-            const uint32_t got = each_free(a.refs, a.n_pages, total, s.w, [&](uint32_t rank, int page) {
+            const uint32_t got = each_free(a.refs, a.n_pages, total, s.w, counts0, [&](uint32_t rank, int page) {
                 if (rank < kFound) found[rank] = page;
             });
             __syncthreads();
@@ -126,7 +138,7 @@ __global__ __launch_bounds__(kBooks) void k_pages_extend(PagesArgs a)
             } else if (total <= kFound) {
                 for (uint32_t rank = tid; rank < total; rank += kBooks) give(rank, found[rank]);
             } else {
-                each_free(a.refs, a.n_pages, total, s.w, give);
+                each_free(a.refs, a.n_pages, total, s.w, counts0, give);
             }
         }
     }
@@ -171,6 +183,7 @@ __global__ __launch_bounds__(kBooks) void k_pages_fork(PagesArgs a, int share)
     __shared__ BooksLds s;
     __shared__ int32_t found[kPagesListed];
     const int tid = threadIdx.x;
+    const Counts counts0(a.refs, a.n_pages, tid * 16);
     for (int i = tid; i < 65536 / 32; i += kBooks) s.seen[i] = 0u;
     if (tid == 0) s.bad = 0u;
     __syncthreads();
@@ -202,7 +215,7 @@ __global__ __launch_bounds__(kBooks) void k_pages_fork(PagesArgs a, int share)
     uint32_t rank = block_exclusive_scan<kBookWaves>((uint32_t)__builtin_popcount(half), s.w, &total);
     uint32_t code = s.bad;
     if (code == 0 && total > 0) {
-        const uint32_t got = each_free(a.refs, a.n_pages, total, s.w, [&](uint32_t r, int page) { found[r] = page; });
+        const uint32_t got = each_free(a.refs, a.n_pages, total, s.w, counts0, [&](uint32_t r, int page) { found[r] = page; });
         if (got < total) code = DS_PAGES_NO_ROOM;
     }
     __syncthreads();
@@ -258,47 +271,51 @@ __global__ __launch_bounds__(kWG) void k_pages_free(PagesArgs a)
     if (tid == 0) a.lens[row] = 0;
 }
 
-// The live pages behind the first n_live go to the free ones among them: see ds_pages_compact.  Leaves where every page went
-// in map.
-__global__ __launch_bounds__(kBooks) void k_pages_compact(PagesArgs a, int32_t *map, int32_t *holes)
+// The live pages behind the first n_live go to the free ones among them: see ds_pages_compact.  Leaves n_live and where
+// those pages went in the workspace: ws[0], and ws[4 + page]; ws[4 + n_pages ..] lists the free ones.
+__global__ __launch_bounds__(kBooks) void k_pages_compact(PagesArgs a, int32_t *ws)
 {
     __shared__ uint32_t s_w[kBookWaves];
     const int tid = threadIdx.x;
-    const uint32_t n_free = each_free(a.refs, a.n_pages, (uint32_t)a.n_pages, s_w, [](uint32_t, int) {});
-    const int n_live = a.n_pages - (int)n_free;
-    const uint32_t n_holes = each_free(a.refs, n_live, (uint32_t)n_live, s_w, [&](uint32_t rank, int page) { holes[rank] = page; });
+    int32_t *map = ws + 4, *holes = map + a.n_pages;
+    const Counts counts0(a.refs, a.n_pages, tid * 16);
+    const int n_live = a.n_pages - (int)each_free(a.refs, a.n_pages, (uint32_t)a.n_pages, s_w, counts0, [](uint32_t, int) {});
+    // holes (free, before n_live) and movers (held, from n_live on), ascending: as many of one as of the other
+    uint32_t n_holes = 0, n_movers = 0;
+    for (int p0 = 0; p0 < a.n_pages; p0 += kBooks * 16) {
+        const int mine = p0 + tid * 16;
+        const uint32_t there = mine + 16 <= a.n_pages ? 0xffffu : mine < a.n_pages ? (1u << (a.n_pages - mine)) - 1u : 0u;
+        const uint32_t front = mine + 16 <= n_live ? 0xffffu : mine < n_live ? (1u << (n_live - mine)) - 1u : 0u;
+        const uint32_t free = p0 == 0 ? counts0.free() : Counts(a.refs, a.n_pages, mine).free();
+        uint32_t hole = free & front, mover = ~free & there & ~front, total;
+        const uint32_t rank = block_exclusive_scan<kBookWaves>((uint32_t)__builtin_popcount(hole) | (uint32_t)__builtin_popcount(mover) << 16, s_w, &total);
+        uint32_t h = n_holes + (rank & 0xffffu), m = n_movers + (rank >> 16);   // (16384 of each in a round at most)
+        for (; hole; hole &= hole - 1u) holes[h++] = mine + __builtin_ctz(hole);
+        for (; mover; mover &= mover - 1u) a.copies[m++].x = mine + __builtin_ctz(mover);
+        n_holes += total & 0xffffu;
+        n_movers += total >> 16;
+    }
     __syncthreads();
-    // movers, ascending, meet the holes, ascending: as many of one as of the other
-    uint32_t have = 0;
-    for (int p0 = 0; p0 < a.n_pages; p0 += kBooks) {
-        const int p = p0 + tid;
-        const bool mover = p >= n_live && p < a.n_pages && a.refs[p] > 0;
-        uint32_t total = 0, rank = 0;
-        if (p0 + kBooks > n_live) {
-            rank = have + block_exclusive_scan<kBookWaves>(mover ? 1u : 0u, s_w, &total);
-            have += total;
-        }
-        int to = p;
-        if (mover) {
-            to = holes[rank];
-            a.copies[rank] = make_int4(p, to, 1 << a.page_log2, 0);
-            a.refs[to] = a.refs[p];
-            a.refs[p] = 0;
-        }
-        if (p < a.n_pages) map[p] = to;
+    for (uint32_t i = tid; i < n_holes; i += kBooks) {
+        const int from = a.copies[i].x, to = holes[i];
+        a.copies[i] = make_int4(from, to, 1 << a.page_log2, 0);
+        map[from] = to;
+        a.refs[to] = a.refs[from];
+        a.refs[from] = 0;
     }
     if (tid == 0) {
+        ws[0] = n_live;
         *a.n_copies = (int32_t)n_holes;
         *a.status = DS_PAGES_DONE;
     }
 }
-__global__ __launch_bounds__(kWG) void k_pages_remap(PagesArgs a, const int32_t *map)
+__global__ __launch_bounds__(kWG) void k_pages_remap(PagesArgs a, const int32_t *ws)
 {
-    const int row = blockIdx.x, held = min(pages_in(a, a.lens[row]), a.max_pages);
+    const int row = blockIdx.x, held = min(pages_in(a, a.lens[row]), a.max_pages), n_live = ws[0];
     int32_t *entry = a.table + (size_t)row * a.max_pages;
     for (int j = blockIdx.y * kWG + threadIdx.x; j < held; j += gridDim.y * kWG) {
         const int p = entry[j];
-        if ((uint32_t)p < (uint32_t)a.n_pages) entry[j] = map[p];
+        if (p >= n_live && p < a.n_pages) entry[j] = ws[4 + p];
     }
 }
 
@@ -356,13 +373,12 @@ hipError_t launch_pages_free(const PagesArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-size_t pages_workspace(int n_pages) { return ((size_t)n_pages * 2 * 4 + 255) / 256 * 256; }
+size_t pages_workspace(int n_pages) { return ((size_t)n_pages * 2 * 4 + 16 + 255) / 256 * 256; }
 
 hipError_t launch_pages_compact(const PagesArgs &a, void *ws, hipStream_t st)
 {
-    auto *map = static_cast<int32_t *>(ws);
-    DS_LAUNCH(KID_PAGES_COMPACT, k_pages_compact, dim3(1), dim3(kBooks), 0, st, a, map, map + a.n_pages);
-    DS_LAUNCH(KID_PAGES_COMPACT, k_pages_remap, dim3(a.n_rows, std::min((a.max_pages + kWG - 1) / kWG, 64)), dim3(kWG), 0, st, a, map);
+    DS_LAUNCH(KID_PAGES_COMPACT, k_pages_compact, dim3(1), dim3(kBooks), 0, st, a, static_cast<int32_t *>(ws));
+    DS_LAUNCH(KID_PAGES_COMPACT, k_pages_remap, dim3(a.n_rows, std::min((a.max_pages + kWG - 1) / kWG, 64)), dim3(kWG), 0, st, a, static_cast<const int32_t *>(ws));
     return hipGetLastError();
 }
 
