@@ -338,7 +338,7 @@ ds_status_t ds_attend_rows(const void *q, const void *KV_rows, float *out,
  * Argument checks: strides are multiples of 8 elements (0: the dense value, Hq * d for q and out, Hkv * d
  * and d for kv_stride and kv_head_stride); q, K, V and out 16-byte aligned, pools of pages 256-byte.
  * n_seqs < 1, total_q < 0, max_kv < 0, bad heads, d != 128, a stride below the row it steps over or
- * beyond 2^30 (kv_head_stride: 2^40), an unknown dtype, or (total_q / 128 + n_seqs) * Hq beyond 2^24 -> DS_ERR_SHAPE.  What is on the device is checked there: a
+ * beyond 2^30 (kv_stride: 2^24, kv_head_stride: 2^40), an unknown dtype, or (total_q / 128 + n_seqs) * Hq beyond 2^24 -> DS_ERR_SHAPE.  What is on the device is checked there: a
  * sequence whose new tokens do not lie in [0, total_q) is not computed (its rows are left as they are), one
  * whose keys do not lie within kv_elems, within its row of the page table or on pages of the pool, or are more than
  * 2^30, gets NaN, and nothing is read outside.

@@ -34,7 +34,7 @@ static bool prompt_ok(const ds_prompt_t *prm, ds_prompt_t *m)
     for (int64_t s : {m->q_stride, m->out_stride, m->kv_stride, m->kv_head_stride})
         if (s % 8 != 0) return false;
     if (m->q_stride < row || m->out_stride < row || m->kv_stride < kD || m->kv_head_stride < kD || m->kv_elems < 0) return false;
-    if (m->q_stride > most || m->out_stride > most || m->kv_stride > most || m->kv_head_stride > 1ll << 40) return false;
+    if (m->q_stride > most || m->out_stride > most || m->kv_stride > 1ll << 24 || m->kv_head_stride > 1ll << 40) return false;
     // (a launch holds 2^32 threads at most, and rows are numbered in 32 bits)
     return ((int64_t)m->total_q / kPromptRows + m->n_seqs) * m->Hq <= 1ll << 24;
 }
@@ -58,9 +58,11 @@ size_t ds_prompt_workspace_bytes(const ds_prompt_t *prm)
 }
 
 static PromptArgs prompt_args(const void *q, const void *K, const void *V, void *out, const int32_t *q_start,
-                              const int32_t *kv_len, const ds_prompt_t &m, const PromptPlan &p)
+                              const int32_t *kv_len, void *workspace, const ds_prompt_t &m, const PromptPlan &p)
 {
     PromptArgs a{};
+    a.part_ml = static_cast<float2 *>(workspace);
+    a.part_acc = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.off_acc);
     a.q = q;
     a.K = K;
     a.V = V;
@@ -73,10 +75,12 @@ static PromptArgs prompt_args(const void *q, const void *K, const void *V, void 
     a.kv_head_stride = m.kv_head_stride;
     a.kv_elems = m.kv_elems;
     a.n_seqs = m.n_seqs;
+    a.Hq = m.Hq;
     a.Hkv = m.Hkv;
     a.G = p.G;
     a.total_q = m.total_q;
     a.n_tiles = p.n_tiles;
+    a.n_split = p.n_split;
     return a;
 }
 
@@ -94,7 +98,7 @@ ds_status_t ds_prompt_attention(const void *q, const void *K, const void *V, voi
         return DS_ERR_ALIGN;
     if (workspace_bytes < p.total) return DS_ERR_WORKSPACE;
     if (m.total_q == 0) return DS_OK;
-    PromptArgs a = prompt_args(q, K, V, out, q_start, kv_len, m, p);
+    PromptArgs a = prompt_args(q, K, V, out, q_start, kv_len, workspace, m, p);
     a.kv_start = kv_start;
     DS_TRY(launch_prompt(a, false, m.dtype, (hipStream_t)stream));
     return DS_OK;
@@ -117,7 +121,7 @@ ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const 
         return DS_ERR_ALIGN;
     if (workspace_bytes < p.total) return DS_ERR_WORKSPACE;
     if (m.total_q == 0) return DS_OK;
-    PromptArgs a = prompt_args(q, K_pages, V_pages, out, q_start, lens, m, p);
+    PromptArgs a = prompt_args(q, K_pages, V_pages, out, q_start, lens, workspace, m, p);
     a.rows = rows;
     a.table = table;
     a.n_pages = pages->n_pages;

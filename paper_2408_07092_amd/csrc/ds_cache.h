@@ -21,6 +21,7 @@ constexpr int kMostTokens = 1 << 30;  // of a sequence: what the kernels step pa
 
 // ---------------------------------------------------------------- prompt attention
 constexpr int kPromptRows = 128;   // rows (token * G + head of the group) of a workgroup
+constexpr int kPromptParts = 64;   // parts that keys are split into at most: a lane of the join for each
 
 struct PromptArgs {
     const void *q, *K, *V;
@@ -28,15 +29,17 @@ struct PromptArgs {
     const int32_t *q_start, *kv_start, *kv_len;   // (paged: kv_len by table row)
     const int32_t *rows, *table;                  // paged only
     int64_t q_stride, out_stride, kv_stride, kv_head_stride, kv_elems;
-    int n_seqs, Hkv, G, total_q, n_tiles;
+    float2 *part_ml;                              // [n_split][total_q][Hq]: maximum and sum of a row over a part of the keys
+    float *part_acc;                              // [n_split][total_q][Hq][d]: its numerator
+    int n_seqs, Hq, Hkv, G, total_q, n_tiles, n_split;
     int n_pages, page_log2, max_pages, n_table;   // paged only
 };
 struct PromptPlan {
-    int G, n_tiles;
-    size_t total;
+    int G, n_tiles, n_split;
+    size_t off_acc, total;
 };
 bool make_prompt_plan(const ds_prompt_t &m, PromptPlan *p);
-hipError_t launch_prompt(PromptArgs a, bool paged, int dtype, hipStream_t st);
+hipError_t launch_prompt(const PromptArgs &a, bool paged, int dtype, hipStream_t st);
 
 // Row tiles of packed sequences, numbered without a prefix sum: sequence s has its tiles from number
 // floor(q_start[s] G / 128) + s on, which leaves room for the part tile that each one may end in.

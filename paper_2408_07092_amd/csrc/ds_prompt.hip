@@ -52,9 +52,8 @@ struct Mma<__bf16> {
 };
 
 // Where the 16-byte piece c of a tile's row r lies in LDS: rows of 256 bytes would put a column of
-// pieces on the same four banks.  K is read a piece of each of 32 rows at a time, V by the
-// transposing read two pieces of each of four rows.
-__device__ __forceinline__ int k_piece(int r, int c) { return r * 16 + (c ^ (r & 15)); }
+// pieces on the same four banks.  Of V, which the transposing read takes two pieces of each of four rows at a time from, at
+// v_piece(r, c); of K, read a piece of each of 32 rows at a time, at r * 16 + (c ^ (r & 15)).
 __device__ __forceinline__ int v_piece(int r, int c) { return r * 16 + (c ^ ((r & 3) << 2)); }
 
 __device__ __forceinline__ float halves_max(float v)
@@ -68,13 +67,13 @@ __device__ __forceinline__ float halves_sum(float v)
     return __uint_as_float(r.x) + __uint_as_float(r.y);
 }
 
-// Sixteen bytes of every lane from memory into LDS, to `at` (bytes, the wavefront's) + 16 lane, past the registers.
-// Written out because the compiler, not knowing which buffer a transposing read reads, would wait for every load
-// in flight ahead of each of them; the loads are waited for by wait_tiles.  (m0, the place in LDS, is used for nothing
-// else in this kernel.)
-__device__ __forceinline__ void load_to_lds(const void *src, uint32_t at)
+// Sixteen bytes of every lane, at base + off bytes, from memory into LDS past the registers: to `at` (bytes, the wavefront's)
+// + 16 lane.  Written out because the compiler, not knowing which buffer a transposing read reads, would wait for every
+// load in flight ahead of each of them; the loads are waited for by wait_tiles.  (m0, the place in LDS, is used for
+// nothing else in this kernel.)
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint32_t at)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(at), "v"(src) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(off), "s"(base) : "memory");
 }
 __device__ __forceinline__ void wait_tiles()
 {
@@ -116,10 +115,15 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         kv0 = kv0 * a.kv_stride + (int64_t)kvh * a.kv_head_stride;
     }
     if (bad) nk = 0;
-    const int before = nk - (qe - qs);               // keys ahead of the sequence's first row's own
     const int last_row = min(n_rows, r0 + kPromptRows) - 1;
-    const int seen = max(0, min(nk, last_row / a.G + before + 1));    // keys that some row of the workgroup sees
-    const int n_kt = (seen + kKeys - 1) / kKeys;
+    const int seen = max(0, min(nk, last_row / a.G + nk - (qe - qs) + 1));    // keys that some row of the workgroup sees
+    // ---- its part of them, where the keys are split; from here on keys count from its first
+    const int all_kt = (seen + kKeys - 1) / kKeys, part_kt = (all_kt + a.n_split - 1) / a.n_split;
+    const int kt0 = min((int)blockIdx.y * part_kt, all_kt), n_kt = min(part_kt, all_kt - kt0);
+    const int first_key = kt0 * kKeys;
+    const int before = nk - (qe - qs) - first_key;   // keys ahead of the sequence's first row's own
+    nk = min(nk - first_key, n_kt * kKeys);
+    if constexpr (!PAGED) kv0 += first_key * a.kv_stride;
     const int my_row = r0 + wave * 32 + lo;
     const bool on = my_row < n_rows;
     const int my_last = on ? min(my_row / a.G + before, nk - 1) : -1; // last key that the lane's row sees
@@ -140,18 +144,18 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     float m = kLeast, l = 0.0f;
 
     // ---- tiles: of each 16 rows a wavefront brings four, a lane one piece.  The pieces of a row change places on the
-    // way (see k_piece), by the lane's place in memory, since in LDS a load's lanes lie side by side.
+    // way (see v_piece), by the lane's place in memory, since in LDS a load's lanes lie side by side.
     // Rows past the last key re-read it (their weight is 0, and 0 times whatever lies behind it need not be).
     const int lane_row = 4 * wave + (lane >> 4);
-    const int64_t step_row = PAGED ? kD : a.kv_stride;
-    const T *Kp = static_cast<const T *>(a.K) + kv0 + lane_row * step_row + ((lane & 15) ^ lane_row) * 8;
-    const T *Vp = static_cast<const T *>(a.V) + kv0 + lane_row * step_row + ((lane & 15) ^ ((lane >> 4) << 2)) * 8;
+    const uint32_t row_bytes = PAGED ? kD * 2 : (uint32_t)a.kv_stride * 2;   // (64 rows are within 2^31 bytes)
+    const uint32_t k_off = ((lane & 15) ^ lane_row) * 16, v_off = ((lane & 15) ^ ((lane >> 4) << 2)) * 16, row_off = lane_row * row_bytes;
+    const T *Kp = static_cast<const T *>(a.K) + kv0, *Vp = static_cast<const T *>(a.V) + kv0;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)tiles + wave * 1024;
     // Paged: lane i % 4 of `of` holds the page of a tile's rows 16 i .. (16 rows that start at a multiple of 16 are in one page)
     auto page_ids = [&](int kt) {
         int p = 0;
         if constexpr (PAGED) {
-            if (nk > 0) p = pages[min(kt * kKeys + (lane & 3) * 16, nk - 1) >> a.page_log2];
+            if (nk > 0) p = pages[(first_key + min(kt * kKeys + (lane & 3) * 16, nk - 1)) >> a.page_log2];
             if ((uint32_t)p >= (uint32_t)a.n_pages) {
                 if (kt < n_kt) bad = true;
                 p = 0;
@@ -159,35 +163,52 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         }
         return p;
     };
-    auto load_tile = [&](const T *base, int kt, int buffer, int of) {
-        const bool full = (kt + 1) * kKeys <= nk;
-        const uint32_t at = lds0 + buffer * kTileBytes;
+    // rows 16 i .. of tile kt: the wavefront's four of them
+    auto load_rows = [&](const T *base, uint32_t off, int kt, int i, int buffer, int of, auto whole) {
+        const int t0 = kt * kKeys + i * 16;
+        const uint32_t at = lds0 + buffer * kTileBytes + i * 4096;
+        if constexpr (PAGED) {
+            const int64_t p = __builtin_amdgcn_readlane(of, i);
+            const int g0 = whole ? t0 : min(t0, nk - 1) & ~15;
+            const T *src = base + (((p * a.Hkv + kvh) << a.page_log2) + ((first_key + g0) & ((1 << a.page_log2) - 1))) * kD;
+            load_to_lds(src, off + (whole ? row_off : (uint32_t)(min(t0 + lane_row, nk - 1) - g0) * row_bytes), at);
+        } else if constexpr (whole) {
+            load_to_lds(base + t0 * a.kv_stride, off + row_off, at);
+        } else {
+            load_to_lds(base + kt * kKeys * a.kv_stride, off + (uint32_t)(min(t0 + lane_row, nk - 1) - kt * kKeys) * row_bytes, at);
+        }
+    };
+    auto load_tile = [&](const T *base, uint32_t off, int kt, int buffer, int of) {
+        if ((kt + 1) * kKeys <= nk) {
 #pragma unroll
-        for (int i = 0; i < kKeys / 16; ++i) {
-            const int t0 = kt * kKeys + i * 16;
-            const T *src = base;
-            if constexpr (PAGED) {
-                const int64_t p = __builtin_amdgcn_readlane(of, i);
-                src += (((p * a.Hkv + kvh) << a.page_log2) + (min(t0, nk - 1) & ((1 << a.page_log2) - 1) & ~15)) * kD;
-                if (full) load_to_lds(src, at + i * 4096);
-                else load_to_lds(src + (min(t0 + lane_row, nk - 1) - (min(t0, nk - 1) & ~15) - lane_row) * kD, at + i * 4096);
-            } else {
-                src += t0 * a.kv_stride;
-                if (full) load_to_lds(src, at + i * 4096);
-                else load_to_lds(src + (int64_t)min(0, nk - 1 - t0 - lane_row) * a.kv_stride, at + i * 4096);
-            }
+            for (int i = 0; i < 4; ++i) load_rows(base, off, kt, i, buffer, of, std::true_type{});
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_rows(base, off, kt, i, buffer, of, std::false_type{});
         }
     };
 
-    auto scores = [&](int buffer, f32x16 (&S)[2]) {
-        const u32x4 *kb = tiles + buffer * kPieces;
+    // S = K Q of a tile; between(x) is done ahead of the x-th pieces' products
+    auto scores = [&](int buffer, f32x16 (&S)[2], auto between) {
+        // (the places of pieces 2 x + hi of row lo are formed anew in every step: eight registers that the loop cannot spare)
+        int at = (lo * 16 + (hi ^ (lo & 15))) * 16;
+        asm volatile("" : "+v"(at));
+        const char *kb = reinterpret_cast<const char *>(tiles + buffer * kPieces);
+        vec8 k[8][2];   // (those of two x at a time are there: read one ahead of their products)
+        auto read = [&](int x) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) k[x][b] = *reinterpret_cast<const vec8 *>(kb + b * 8192 + (at ^ x * 32));
+        };
 #pragma unroll
         for (int b = 0; b < 2; ++b) S[b] = (f32x16)(0.0f);
+        read(0);
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
+        for (int x = 0; x < 8; ++x) {
+            if (x < 7) read(x + 1);
+            between(x);
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-                S[b] = Mma<T>::dot(__builtin_bit_cast(vec8, kb[k_piece(b * 32 + lo, 2 * x + hi)]), q[x], S[b]);
+            for (int b = 0; b < 2; ++b) S[b] = Mma<T>::dot(k[x][b], q[x], S[b]);
+        }
     };
     auto hide = [&](int kt, f32x16 (&S)[2]) {
         const int left = my_last - kt * kKeys - 4 * hi;
@@ -249,15 +270,15 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
 
     int ids0 = page_ids(0), ids1 = page_ids(1);
     if (n_kt > 0) {
-        load_tile(Kp, 0, 0, ids0);
-        load_tile(Vp, 0, 2, ids0);
-        if (n_kt > 1) load_tile(Kp, 1, 1, ids1);
+        load_tile(Kp, k_off, 0, 0, ids0);
+        load_tile(Vp, v_off, 0, 2, ids0);
+        if (n_kt > 1) load_tile(Kp, k_off, 1, 1, ids1);
     }
     ids0 = page_ids(2);
     wait_tiles();
     f32x16 S0[2], S1[2];
     if (n_mine > 0) {
-        scores(0, S0);
+        scores(0, S0, [](int) {});
         if (n_clear < 1) hide(0, S0);
         raise(S0);
     }
@@ -265,17 +286,29 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     // values, with the sum of the weights and the next one's maximum (so that both halves have vector work, and registers do); the K tile after the next and the next V tile are on their way meanwhile, to
     // places whose tiles were done with before the last barrier.  odd: kt % 2
     auto bring = [&](int kt, int odd) {
-        if (kt + 1 < n_kt) load_tile(Vp, kt + 1, 3 - odd, ids1);
-        if (kt + 2 < n_kt) load_tile(Kp, kt + 2, odd, ids0);
+        if (kt + 1 < n_kt) load_tile(Vp, v_off, kt + 1, 3 - odd, ids1);
+        if (kt + 2 < n_kt) load_tile(Kp, k_off, kt + 2, odd, ids0);
         ids1 = ids0;
         ids0 = page_ids(kt + 3);
     };
     auto step = [&](int kt, int odd, f32x16 (&S)[2], f32x16 (&N)[2], auto hidden) {
-        bring(kt, odd);
         vec8 P[4];
-        scores(1 - odd, N);
+        if constexpr (hidden) {
+            bring(kt, odd);
+            scores(1 - odd, N, [](int) {});
+        } else {
+            // (Whole tiles, as all but the last: one load at a time between the products.  The eight of them in a row ahead of
+            //  the step kept the wavefront from its products for as long as they take to be accepted: 8K tokens of 32 heads
+            //  581 -> 531 us, two of 8K in groups of 4 1073 -> 977, 512 on 20K in groups of 8 697 -> 638.)
+            scores(1 - odd, N, [&](int x) {
+                if (x < 4) load_rows(Vp, v_off, kt + 1, x, 3 - odd, ids1, std::true_type{});
+                else load_rows(Kp, k_off, kt + 2, x - 4, odd, ids0, std::true_type{});
+            });
+            ids1 = ids0;
+            ids0 = page_ids(kt + 3);
+        }
         weights(S, P, 0, 3);
-        if (hidden) hide(kt + 1, N);
+        if constexpr (hidden) hide(kt + 1, N);
         values(odd, P, 0, 3);
         weights(S, P, 3, 4);
         values(odd, P, 3, 4);
@@ -284,7 +317,7 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         wait_tiles();
     };
     int kt = 0;
-    for (; kt + 2 < n_clear; kt += 2) {
+    for (const int n_whole = nk / kKeys; kt + 2 < n_clear && kt + 3 < n_whole; kt += 2) {
         step(kt, 0, S0, S1, std::false_type{});
         step(kt + 1, 1, S1, S0, std::false_type{});
     }
@@ -313,9 +346,23 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     }
     if (!on) return;
     l = halves_sum(l);
-    // (a row that sees no key is zero; one whose pages or places are not there is NaN)
-    const float inv = bad ? __builtin_nanf("") : l > 0.0f ? 1.0f / l : 0.0f;
-    T *dst = static_cast<T *>(a.out) + (size_t)(qs + my_row / a.G) * a.out_stride + (size_t)(kvh * a.G + my_row % a.G) * kD + 4 * hi;
+    if (bad) l = __builtin_nanf("");                 // (a row whose pages or places are not there is NaN ...
+    const int64_t token = qs + my_row / a.G;
+    const int head = kvh * a.G + my_row % a.G;
+    if (a.n_split > 1) {
+        const int64_t row = ((int64_t)blockIdx.y * a.total_q + token) * a.Hq + head;
+        if (hi == 0) a.part_ml[row] = make_float2(m, l);
+        if (l == 0.0f) return;                       // (a part without a key that the row sees)
+        float *acc = a.part_acc + row * kD + 4 * hi;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4 *>(acc + d * 32 + i * 8) = (f32x4){O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]};
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // ... one that sees no key is zero)
+    T *dst = static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 4 * hi;
     typedef T vec4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -328,12 +375,73 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         }
 }
 
+// Joins the parts of split keys, a wavefront for a row of a head:
+//   y = sum_z acc_z 2^(m_z - M) / sum_z l_z 2^(m_z - M),  M = max_z m_z,  z ascending.
+template <class T>
+__global__ __launch_bounds__(kWG) void k_prompt_join(PromptArgs a)
+{
+    typedef T vec2 __attribute__((ext_vector_type(2)));
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)a.total_q * a.Hq;
+    const int64_t row = (int64_t)blockIdx.x * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row >= rows) return;
+    const int token = (int)(row / a.Hq), head = (int)(row % a.Hq);
+    const int s = last_at_or_before(a.n_seqs, token, [&](int i) { return a.q_start[i]; });
+    const int qs = a.q_start[s], qe = a.q_start[s + 1];
+    if (qs < 0 || qe < qs || qe > a.total_q || token < qs || token >= qe) return;   // (no row of a sequence: left as it is)
+    const float2 ml = lane < a.n_split ? a.part_ml[lane * rows + row] : make_float2(kLeast, 0.0f);
+    float M = ml.x;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    const float f = __builtin_amdgcn_exp2f(ml.x - M);
+    float L = f * ml.y;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o);
+    const uint64_t there = __ballot(ml.y != 0.0f);   // parts that have written a numerator
+    float2 A = make_float2(0.0f, 0.0f);
+    constexpr int kFlight = 8;
+    for (int z0 = 0; z0 < a.n_split; z0 += kFlight) {
+        float2 v[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const bool on = z0 + i < a.n_split && (there >> (z0 + i) & 1u);
+            v[i] = on ? *reinterpret_cast<const float2 *>(a.part_acc + ((z0 + i) * rows + row) * kD + 2 * lane) : make_float2(0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const float w = __shfl(f, (z0 + i) & 63);
+            A.x += w * v[i].x;
+            A.y += w * v[i].y;
+        }
+    }
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    *reinterpret_cast<vec2 *>(static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 2 * lane) = (vec2){(T)(A.x * inv), (T)(A.y * inv)};
+}
+
 // ---------------------------------------------------------------- launcher
 bool make_prompt_plan(const ds_prompt_t &m, PromptPlan *p)
 {
     p->G = m.Hq / m.Hkv;
     p->n_tiles = (int)((int64_t)m.total_q * p->G / kPromptRows) + m.n_seqs;
-    p->total = 256;
+    p->n_split = 1;
+    // Few rows over many keys: the keys are split, until two workgroups to a compute unit have work at most.  A part
+    // saves its share of the steps, 1.2 us each (one workgroup's step is latency), and costs a numerator of every row,
+    // written and read, and the join about 4 us.  (us, not split and split: 16 tokens on 30000, groups of 4, 818 -> 39; eight of
+    // 16 on 2000 63 -> 31; two of 60 on 10000, single heads 237 -> 80; on the other side of the line 500 tokens 18 -> 24 in two
+    // parts, 1000 in groups of 7 30 -> 42.)
+    const int64_t wgs = (int64_t)p->n_tiles * m.Hkv, most = std::min<int64_t>(2 * device_caps().cus / wgs, kPromptParts);
+    const double steps = 1.2 * m.max_kv / kKeys, row_part = (double)m.total_q * m.Hq * (2 * kD * 4) / 3e6;
+    double best = steps;
+    for (int n = 2; n <= most; ++n) {
+        const double us = steps / n + 4.0 + n * row_part;
+        if (us < best) {
+            best = us;
+            p->n_split = n;
+        }
+    }
+    const size_t rows = (size_t)m.total_q * m.Hq * p->n_split;
+    p->off_acc = p->n_split > 1 ? (rows * 8 + 255) / 256 * 256 : 0;
+    p->total = p->off_acc + (p->n_split > 1 ? rows * kD * 4 : 256);
     return true;
 }
 
@@ -344,10 +452,15 @@ static PromptFn prompt_fn(bool paged, int dtype)
     return paged ? k_prompt<_Float16, true> : k_prompt<_Float16, false>;
 }
 
-hipError_t launch_prompt(PromptArgs a, bool paged, int dtype, hipStream_t st)
+hipError_t launch_prompt(const PromptArgs &a, bool paged, int dtype, hipStream_t st)
 {
     const PromptFn fn = prompt_fn(paged, dtype);
-    DS_LAUNCH(KID_PROMPT, fn, dim3((unsigned)(a.n_tiles * a.Hkv)), dim3(kWG), 4 * kTileBytes, st, a);
+    DS_LAUNCH(KID_PROMPT, fn, dim3((unsigned)(a.n_tiles * a.Hkv), a.n_split), dim3(kWG), 4 * kTileBytes, st, a);
+    if (a.n_split > 1) {
+        const unsigned wgs = (unsigned)(((int64_t)a.total_q * a.Hq + kWG / 64 - 1) / (kWG / 64));
+        const PromptFn join = dtype == DS_BF16 ? k_prompt_join<__bf16> : k_prompt_join<_Float16>;
+        DS_LAUNCH(KID_PROMPT, join, dim3(wgs), dim3(kWG), 0, st, a);
+    }
     return hipGetLastError();
 }
 

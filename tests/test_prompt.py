@@ -41,7 +41,7 @@ def test_refusals():
     assert call(None) == ds.DS_ERR_NULL
     for bad in (dict(n_seqs=0), dict(total_q=-1), dict(max_kv=-1), dict(Hq=7), dict(Hkv=0), dict(Hq=0), dict(d=64), dict(dtype=2),
                 dict(dtype=-1), dict(q_stride=8 * D - 8), dict(q_stride=8 * D + 4), dict(out_stride=4), dict(kv_stride=120),
-                dict(kv_stride=D + 1), dict(kv_head_stride=8), dict(kv_elems=-1), dict(kv_stride=(1 << 30) + 8),
+                dict(kv_stride=D + 1), dict(kv_head_stride=8), dict(kv_elems=-1), dict(kv_stride=(1 << 24) + 8),
                 dict(q_stride=-8 * D), dict(kv_head_stride=(1 << 40) + 8), dict(total_q=2**31 - 1), dict(n_seqs=1 << 22)):
         assert call(ds.prompt(**{**GOOD, **bad})) == ds.DS_ERR_SHAPE, bad
         assert ds.ds_prompt_workspace_bytes(ds.prompt(**{**GOOD, **bad})) == 0
@@ -185,6 +185,57 @@ def test_strided_layouts(layout, dtype):
     assert (out_wide[:, 0] == CANARY).all() and (out_wide[:, -1] == CANARY).all()
     for i, (k, v) in enumerate(rows):
         near(out[int(qs[i]):int(qs[i + 1])], q[int(qs[i]):int(qs[i + 1])], k, v, before[i], t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("guide", [0, 700, 5000, 200000])
+def test_split_keys(guide, dtype):
+    """Few rows: the keys are split by the length that is told, whatever the true ones are -- parts with one key, with none
+    that a row sees, and none at all -- and joined; a bad place is NaN through the join, and the others are whole."""
+    t, code = TYPES[dtype]
+    Hq, Hkv, P = 8, 2, 32
+    new, before = [3, 1, 0, 20, 2, 65], [4000, 0, 3, -5, 64, 63]
+    keys = [a + b for a, b in zip(new, before)]
+    T, R = sum(new) + 3, sum(keys)
+    q, K, V = values((T, Hq, D), t, 1).cuda(), values((R, Hkv, D), t, 2, True).cuda(), values((R, Hkv, D), t, 3).cuda()
+    qs, ks = starts(new, 1), starts(keys)
+    prm = ds.prompt(len(new), Hq, Hkv, D, T, guide, code, kv_elems=K.numel())
+    ws = ds.ds_prompt_workspace_alloc(prm)
+    assert (ws.numel() > 256) == (guide > 0)                    # (there are parts)
+    for broken in (False, True):
+        lens = torch.tensor(keys, dtype=torch.int32)
+        if broken:
+            lens[3] = R + 1
+        out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+        ds.ds_prompt_attention(q, K, V, out, qs.cuda(), ks[:-1].contiguous().cuda(), lens.cuda(), ws, prm)
+        torch.cuda.synchronize()
+        assert (out[0] == CANARY).all() and (out[1 + sum(new):] == CANARY).all()
+        for i, (m, n, b) in enumerate(zip(new, keys, before)):
+            o, r = int(qs[i]), int(ks[i])
+            if broken and i == 3:
+                assert torch.isnan(out[o:o + m]).all()
+                continue
+            near(out[o:o + m], q[o:o + m], K[r:r + n], V[r:r + n], b, t)
+            if b < 0:
+                assert (out[o:o - b] == 0).all()
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 21)
+    rows, lens = torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda(), torch.tensor([9] + keys + [9], dtype=torch.int32).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    for bad in (None, Kp.shape[0], -1):
+        tb = table.clone()
+        if bad is not None:
+            tb[1, 70] = bad                                     # in the middle of the long one
+        out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+        ds.ds_prompt_attention_paged(q, Kp, Vp, out, qs.cuda(), rows, lens, tb, ws, prm, pg)
+        torch.cuda.synchronize()
+        assert (out[0] == CANARY).all() and (out[1 + sum(new):] == CANARY).all()
+        for i, (m, b) in enumerate(zip(new, before)):
+            o = int(qs[i])
+            if bad is not None and i == 0:
+                assert torch.isnan(out[o:o + m]).all()
+            else:
+                near(out[o:o + m], q[o:o + m], kv[i][0], kv[i][1], b, t)
 
 
 def paged(keys, Hkv, P, t, seed, spare=3):
