@@ -293,20 +293,17 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     };
     auto step = [&](int kt, int odd, f32x16 (&S)[2], f32x16 (&N)[2], auto hidden) {
         vec8 P[4];
-        if constexpr (hidden) {
-            bring(kt, odd);
-            scores(1 - odd, N, [](int) {});
-        } else {
-            // (Whole tiles, as all but the last: one load at a time between the products.  The eight of them in a row ahead of
-            //  the step kept the wavefront from its products for as long as they take to be accepted: 8K tokens of 32 heads
-            //  581 -> 531 us, two of 8K in groups of 4 1073 -> 977, 512 on 20K in groups of 8 697 -> 638.)
-            scores(1 - odd, N, [&](int x) {
-                if (x < 4) load_rows(Vp, v_off, kt + 1, x, 3 - odd, ids1, std::true_type{});
-                else load_rows(Kp, k_off, kt + 2, x - 4, odd, ids0, std::true_type{});
-            });
-            ids1 = ids0;
-            ids0 = page_ids(kt + 3);
-        }
+        // (One load at a time between the products.  The eight of them in a row ahead of the step kept the wavefront from
+        //  its products for as long as they take to be accepted: 8K tokens of 32 heads 581 -> 531 us, two of 8K in groups
+        //  of 4 1073 -> 977, 512 on 20K in groups of 8 697 -> 638.  Behind the last K tile it comes again, to a place
+        //  that nobody reads.)
+        scores(1 - odd, N, [&](int x) {
+            constexpr std::bool_constant<!hidden> whole{};
+            if (x < 4) load_rows(Vp, v_off, kt + 1, x, 3 - odd, ids1, whole);
+            else load_rows(Kp, k_off, hidden ? min(kt + 2, n_kt - 1) : kt + 2, x - 4, odd, ids0, whole);
+        });
+        ids1 = ids0;
+        ids0 = page_ids(kt + 3);
         weights(S, P, 0, 3);
         if constexpr (hidden) hide(kt + 1, N);
         values(odd, P, 0, 3);
