@@ -28,6 +28,7 @@ namespace ds {
 constexpr float kPromptScale = 1.4426950408889634f * 0.08838834764831845f;  // log2(e) / sqrt(128)
 constexpr int kKeys = 64;                                  // keys of a tile
 constexpr int kTileBytes = kKeys * kD * 2;
+constexpr int kAheadK = 2, kAheadV = 4;                    // LDS is read so many pairs of products, or products, ahead of them
 // The running maximum is raised only when a row's exceeds it by more than this (in the log2 domain), so
 // that most tiles rescale nothing; weights carry the factor 2^kRoom besides, which cancels in the quotient.  They
 // are at most 2^(7 + 8), within fp16, and normal fp16 numbers down to 2^-21 of the row's largest.
@@ -188,26 +189,33 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         }
     };
 
+    // Products and LDS reads keep the places that they have here; what the vector units do may move between them.  (Left
+    // to itself the compiler reads right before it multiplies.  1500 tokens of 32 heads 44.0 -> 41.5 us, 500 in groups
+    // of 4 16.4 -> 15.3.)
+    auto pin = []() { __builtin_amdgcn_sched_barrier(0x2 | 0x4 | 0x400); };
     // S = K Q of a tile; between(x) is done ahead of the x-th pieces' products
     auto scores = [&](int buffer, f32x16 (&S)[2], auto between) {
         // (the places of pieces 2 x + hi of row lo are formed anew in every step: eight registers that the loop cannot spare)
         int at = (lo * 16 + (hi ^ (lo & 15))) * 16;
         asm volatile("" : "+v"(at));
         const char *kb = reinterpret_cast<const char *>(tiles + buffer * kPieces);
-        vec8 k[8][2];   // (those of two x at a time are there: read one ahead of their products)
+        vec8 k[8][2];
         auto read = [&](int x) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) k[x][b] = *reinterpret_cast<const vec8 *>(kb + b * 8192 + (at ^ x * 32));
         };
 #pragma unroll
         for (int b = 0; b < 2; ++b) S[b] = (f32x16)(0.0f);
-        read(0);
+#pragma unroll
+        for (int x = 0; x < kAheadK; ++x) read(x);
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
-            if (x < 7) read(x + 1);
+            if (x + kAheadK < 8) read(x + kAheadK);
             between(x);
+            pin();
 #pragma unroll
             for (int b = 0; b < 2; ++b) S[b] = Mma<T>::dot(k[x][b], q[x], S[b]);
+            pin();
         }
     };
     auto hide = [&](int kt, f32x16 (&S)[2]) {
@@ -232,21 +240,28 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
 #pragma unroll
             for (int j = 0; j < 8; j += 2) l = Mma<T>::add2((typename Mma<T>::vec2){P[c][j], P[c][j + 1]}, l);
     };
-    auto values = [&](int buffer, const vec8 (&P)[4], int c0 = 0, int c1 = 4) {
+    // the V operand of products i = 4 c + d: keys 16 c .., channels 32 d ..
+    auto read_v = [&](int buffer, int i) {
         const u32x4 *vb = tiles + (2 + buffer) * kPieces;
+        const int c = i / 4, d = i % 4;
+        // four keys by sixteen channels for each 16 lanes: lane 4 j + x brings row j, channels 4 x ..
+        const int r = 16 * c + 4 * hi + (lane & 15) / 4, piece = d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2;
+        const char *v0 = reinterpret_cast<const char *>(vb + v_piece(r, piece)) + (lane & 1) * 8;
+        const char *v1 = reinterpret_cast<const char *>(vb + v_piece(r + 8, piece)) + (lane & 1) * 8;
+        const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v0);
+        const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v1);
+        const s16x8 v = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+        return __builtin_bit_cast(vec8, v);
+    };
+    auto values = [&](int buffer, vec8 (&v)[kAheadV], const vec8 (&P)[4], int i0, int i1) {
 #pragma unroll
-        for (int c = c0; c < c1; ++c)
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                // four keys by sixteen channels for each 16 lanes: lane 4 j + x brings row j, channels 4 x ..
-                const int r = 16 * c + 4 * hi + (lane & 15) / 4, piece = d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2;
-                const char *v0 = reinterpret_cast<const char *>(vb + v_piece(r, piece)) + (lane & 1) * 8;
-                const char *v1 = reinterpret_cast<const char *>(vb + v_piece(r + 8, piece)) + (lane & 1) * 8;
-                const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v0);
-                const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v1);
-                const s16x8 v = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
-                O[d] = Mma<T>::dot(__builtin_bit_cast(vec8, v), P[c], O[d]);
-            }
+        for (int i = i0; i < i1; ++i) {
+            const vec8 now = v[i % kAheadV];
+            if (i + kAheadV < 16) v[i % kAheadV] = read_v(buffer, i + kAheadV);
+            pin();
+            O[i % 4] = Mma<T>::dot(now, P[i / 4], O[i % 4]);
+            pin();
+        }
     };
     auto raise = [&](const f32x16 (&S)[2]) {
         float top = kNegInf;
@@ -292,7 +307,7 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         ids0 = page_ids(kt + 3);
     };
     auto step = [&](int kt, int odd, f32x16 (&S)[2], f32x16 (&N)[2], auto hidden) {
-        vec8 P[4];
+        vec8 P[4], v[kAheadV];
         // (One load at a time between the products.  The eight of them in a row ahead of the step kept the wavefront from
         //  its products for as long as they take to be accepted: 8K tokens of 32 heads 581 -> 531 us, two of 8K in groups
         //  of 4 1073 -> 977, 512 on 20K in groups of 8 697 -> 638.  Behind the last K tile it comes again, to a place
@@ -301,14 +316,17 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
             constexpr std::bool_constant<!hidden> whole{};
             if (x < 4) load_rows(Vp, v_off, kt + 1, x, 3 - odd, ids1, whole);
             else load_rows(Kp, k_off, hidden ? min(kt + 2, n_kt - 1) : kt + 2, x - 4, odd, ids0, whole);
+            if (x == 7)
+#pragma unroll
+                for (int i = 0; i < kAheadV; ++i) v[i] = read_v(odd, i);
         });
         ids1 = ids0;
         ids0 = page_ids(kt + 3);
         weights(S, P, 0, 3);
         if constexpr (hidden) hide(kt + 1, N);
-        values(odd, P, 0, 3);
+        values(odd, v, P, 0, 12);
         weights(S, P, 3, 4);
-        values(odd, P, 3, 4);
+        values(odd, v, P, 12, 16);
         add_up(P);
         raise(N);
         wait_tiles();
@@ -326,9 +344,11 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     for (; kt < n_kt; ++kt) {   // (the wavefront's last tile, and those that only others see)
         bring(kt, kt & 1);
         if (kt < n_mine) {
-            vec8 P[4];
+            vec8 P[4], v[kAheadV];
+#pragma unroll
+            for (int i = 0; i < kAheadV; ++i) v[i] = read_v(kt & 1, i);
             weights(S0, P);
-            values(kt & 1, P);
+            values(kt & 1, v, P, 0, 16);
             add_up(P);
         }
         wait_tiles();
