@@ -338,10 +338,13 @@ ds_status_t ds_attend_rows(const void *q, const void *KV_rows, float *out,
  * Argument checks: strides are multiples of 8 elements (0: the dense value, Hq * d for q and out, Hkv * d
  * and d for kv_stride and kv_head_stride); q, K, V and out 16-byte aligned, pools of pages 256-byte.
  * n_seqs < 1, total_q < 0, max_kv < 0, bad heads, d != 128, a stride below the row it steps over or
- * beyond 2^30 (kv_stride: 2^24, kv_head_stride: 2^40), an unknown dtype, or (total_q / 128 + n_seqs) * Hq beyond 2^24 -> DS_ERR_SHAPE.  What is on the device is checked there: a
- * sequence whose new tokens do not lie in [0, total_q) is not computed (its rows are left as they are), one
- * whose keys do not lie within kv_elems, within its row of the page table or on pages of the pool, or are more than
- * 2^30, gets NaN, and nothing is read outside.
+ * beyond 2^30 (kv_stride: 2^24, kv_head_stride: 2^40), an unknown dtype, or (total_q / 128 + n_seqs) * Hq of
+ * 2^24 or more -> DS_ERR_SHAPE.  What is on the device is checked there: a sequence whose new tokens do not
+ * lie in [0, total_q) is not computed (its rows are left as they are), one whose keys do not lie within kv_elems,
+ * within its row of the page table or on pages of the pool, or are more than 2^30, gets NaN, and nothing is
+ * read outside.
+ * Keys that a row does not see have no part in it, whatever they and their values hold, infinities and NaN
+ * too; a row that sees such a value takes a slow path, a key at a time.
  * max_kv: keys of the longest sequence (a guide to the split, which the results do not rest on).
  */
 typedef enum { DS_F16 = 0, DS_BF16 = 1 } ds_dtype_t; /* IEEE binary16; bfloat16 */
@@ -404,7 +407,7 @@ ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pa
  * total_new of them) become tokens start[s], start[s] + 1, .. of table row rows[s] (NULL: row s).  new_start
  * [n_seqs + 1], start [n_seqs] int32 on the device; start[s] < 0: nothing is written for s.  The pages have to be in the table
  * (ds_pages_extend); what has no page of the pool is not written.  Rows are distinct.  total_new * ceil(Hkv / 8)
- * at most 2^26, else DS_ERR_SHAPE.
+ * is less than 2^26, else DS_ERR_SHAPE.
  */
 ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages, void *V_pages,
                             const int32_t *new_start, const int32_t *rows, const int32_t *start,

@@ -19,6 +19,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMostTokens = 1 << 30;  // of a sequence: what the kernels step past its end stays within 32 bits
 
+// A running maximum before any score, and where every score is -infinity: what is folded in later takes its weight
+// away (2^(kLeast - m) = 0), and the weights of scores of -infinity are 0, not 2^(-inf + inf).
+constexpr float kLeast = -3e38f;
+
 // ---------------------------------------------------------------- prompt attention
 constexpr int kPromptRows = 128;   // rows (token * G + head of the group) of a workgroup
 constexpr int kPromptParts = 64;   // parts that keys are split into at most: a lane of the join for each

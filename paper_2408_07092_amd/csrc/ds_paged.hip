@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
             q[i] = (vec8)(T)0;
             if (lo < n_heads) q[i] = *reinterpret_cast<const vec8 *>(static_cast<const T *>(a.q) + (head0 + lo) * kD + 8 * (4 * i + hi));
         }
-        float m = kNegInf, l = 0.0f;
+        float m = kLeast, l = 0.0f;
         f32x4 O[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) O[e] = (f32x4)(0.0f);
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
                     if (t + 4 * hi + r >= n) rows.v[r] = (vec8)(T)0;
             }
             const float mn = fmaxf(m, rows_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));  // (token t is there)
-            const float sc = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+            const float sc = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
             float p[4];
 #pragma unroll

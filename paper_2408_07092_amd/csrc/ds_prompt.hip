@@ -33,7 +33,6 @@ constexpr int kAheadK = 2, kAheadV = 4;                    // LDS is read so man
 // that most tiles rescale nothing; weights carry the factor 2^kRoom besides, which cancels in the quotient.  They
 // are at most 2^(7 + 8), within fp16, and normal fp16 numbers down to 2^-21 of the row's largest.
 constexpr float kSlack = 8.0f, kRoom = 7.0f;
-constexpr float kLeast = -1e30f;                           // stands for "no key yet": 2^(s - kLeast) is never formed
 
 template <class T>
 struct Mma;
@@ -80,6 +79,50 @@ __device__ __forceinline__ void wait_tiles()
 {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
+}
+
+// One row of a head anew, a key at a time, over its keys 0 .. last: at(j) is the element of key j's row.  The wavefront
+// takes 64 keys at once for the scores, a lane each, and two channels a lane for the values.  Weights are
+// 2^(s - m) here, so sums of finite values overflow only where the values themselves nearly do.
+template <class T, class At>
+__device__ __forceinline__ void row_alone(const T *q, const T *K, const T *V, int last, At at, float *m, float *l, float2 *A)
+{
+    typedef typename Mma<T>::vec8 vec8;
+    typedef T vec2 __attribute__((ext_vector_type(2)));
+    const int lane = threadIdx.x & 63;
+    *m = last < 0 ? kNegInf : kLeast;
+    *l = 0.0f;
+    *A = make_float2(0.0f, 0.0f);
+    for (int t0 = 0; t0 <= last; t0 += 64) {
+        const T *k = K + at(min(t0 + lane, last));
+        float s = 0.0f;
+#pragma unroll 1
+        for (int x = 0; x < kD; x += 8) {
+            const vec8 kx = *reinterpret_cast<const vec8 *>(k + x), qx = *reinterpret_cast<const vec8 *>(q + x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s = __builtin_fmaf((float)kx[j], (float)qx[j], s);
+        }
+        s = t0 + lane <= last ? s * kPromptScale : kNegInf;
+        float top = s;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+        top = fmaxf(top, *m);
+        const float f = __builtin_amdgcn_exp2f(*m - top), p = __builtin_amdgcn_exp2f(s - top);
+        float sum = p;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        *m = top;
+        *l = *l * f + sum;
+        A->x *= f;
+        A->y *= f;
+#pragma unroll 1
+        for (int i = 0; i < min(64, last - t0 + 1); ++i) {
+            const vec2 v = *reinterpret_cast<const vec2 *>(V + at(t0 + i) + 2 * lane);
+            const float w = __shfl(p, i);
+            A->x += w * (float)v[0];
+            A->y += w * (float)v[1];
+        }
+    }
 }
 
 template <class T, bool PAGED>
@@ -361,35 +404,74 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         __syncthreads();
         bad = *flag != 0u;
     }
-    if (!on) return;
-    l = halves_sum(l);
-    if (bad) l = __builtin_nanf("");                 // (a row whose pages or places are not there is NaN ...
-    const int64_t token = qs + my_row / a.G;
-    const int head = kvh * a.G + my_row % a.G;
-    if (a.n_split > 1) {
-        const int64_t row = ((int64_t)blockIdx.y * a.total_q + token) * a.Hq + head;
-        if (hi == 0) a.part_ml[row] = make_float2(m, l);
-        if (l == 0.0f) return;                       // (a part without a key that the row sees)
-        float *acc = a.part_acc + row * kD + 4 * hi;
+    if (on) {
+        l = halves_sum(l);
+        const int64_t token = qs + my_row / a.G;
+        const int head = kvh * a.G + my_row % a.G;
+        if (a.n_split > 1) {
+            const int64_t row = ((int64_t)blockIdx.y * a.total_q + token) * a.Hq + head;
+            if (my_last < 0) m = kNegInf;                // (a part without a key that the row sees)
+            if (hi == 0) a.part_ml[row] = bad ? make_float2(0.0f, __builtin_nanf("")) : make_float2(m, l);
+            if (l != 0.0f) {
+                float *acc = a.part_acc + row * kD + 4 * hi;
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+                for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<f32x4 *>(acc + d * 32 + i * 8) = (f32x4){O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]};
-        return;
-    }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // ... one that sees no key is zero)
-    T *dst = static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 4 * hi;
-    typedef T vec4 __attribute__((ext_vector_type(4)));
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32x4 *>(acc + d * 32 + i * 8) = (f32x4){O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]};
+            }
+        } else {
+            // (a row whose pages or places are not there is NaN, one that sees no key is zero)
+            const float inv = bad ? __builtin_nanf("") : my_last < 0 ? 0.0f : 1.0f / l;
+            T *dst = static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 4 * hi;
+            typedef T vec4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            vec4 x;
+                for (int i = 0; i < 4; ++i) {
+                    vec4 x;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = (T)(O[d][4 * i + j] * inv);
-            *reinterpret_cast<vec4 *>(dst + d * 32 + i * 8) = x;
+                    for (int j = 0; j < 4; ++j) x[j] = (T)(O[d][4 * i + j] * inv);
+                    *reinterpret_cast<vec4 *>(dst + d * 32 + i * 8) = x;
+                }
         }
+    }
+    // A value that is not finite comes into rows that do not see its key as well, 0 times it being NaN.  So rows whose
+    // numerator is not finite are formed anew without the matrix units, from the keys that they see.  (Nor does it
+    // matter then that the numerator of a row of huge values had overflowed.)  Looked at while the rows above are being written.
+    f32x16 all = (O[0] + O[1]) + (O[2] + O[3]);
+#pragma unroll
+    for (int n = 8; n > 0; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) all[i] += all[i + n];
+    const uint64_t beyond = __ballot(on && !bad && !(fabsf(all[0]) < __builtin_inff()));
+    const uint32_t anew = (uint32_t)beyond | (uint32_t)(beyond >> 32);
+    if (anew) __threadfence();   // (they are written once more)
+    for (uint32_t left = anew; left; left &= left - 1u) {
+        const int row = r0 + wave * 32 + __builtin_ctz(left), head = kvh * a.G + row % a.G;
+        const int64_t token = qs + row / a.G;
+        auto at = [&](int j) -> int64_t {
+            if constexpr (PAGED) {
+                const int t = first_key + j;
+                return ((((int64_t)pages[t >> a.page_log2] * a.Hkv + kvh) << a.page_log2) + (t & ((1 << a.page_log2) - 1))) * kD;
+            } else {
+                return kv0 + j * a.kv_stride;
+            }
+        };
+        const int last = min(row / a.G + before, nk - 1);
+        float m1, l1;
+        float2 A;
+        row_alone(static_cast<const T *>(a.q) + token * a.q_stride + (int64_t)head * kD, static_cast<const T *>(a.K),
+                  static_cast<const T *>(a.V), last, at, &m1, &l1, &A);
+        if (a.n_split > 1) {
+            const int64_t to = ((int64_t)blockIdx.y * a.total_q + token) * a.Hq + head;
+            if (lane == 0) a.part_ml[to] = make_float2(m1 + kRoom, l1);    // (2^(s - m) is 2^(s - (m + kRoom) + kRoom))
+            *reinterpret_cast<float2 *>(a.part_acc + to * kD + 2 * lane) = A;
+        } else {
+            typedef T vec2 __attribute__((ext_vector_type(2)));
+            *reinterpret_cast<vec2 *>(static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 2 * lane) = last < 0 ? (vec2)(T)0.0f : (vec2){(T)(A.x / l1), (T)(A.y / l1)};
+        }
+    }
 }
 
 // Joins the parts of split keys, a wavefront for a row of a head:
@@ -406,11 +488,11 @@ __global__ __launch_bounds__(kWG) void k_prompt_join(PromptArgs a)
     const int s = last_at_or_before(a.n_seqs, token, [&](int i) { return a.q_start[i]; });
     const int qs = a.q_start[s], qe = a.q_start[s + 1];
     if (qs < 0 || qe < qs || qe > a.total_q || token < qs || token >= qe) return;   // (no row of a sequence: left as it is)
-    const float2 ml = lane < a.n_split ? a.part_ml[lane * rows + row] : make_float2(kLeast, 0.0f);
+    const float2 ml = lane < a.n_split ? a.part_ml[lane * rows + row] : make_float2(kNegInf, 0.0f);
     float M = ml.x;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    const float f = __builtin_amdgcn_exp2f(ml.x - M);
+    const float f = ml.x == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(ml.x - M);
     float L = f * ml.y;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o);
@@ -431,7 +513,7 @@ __global__ __launch_bounds__(kWG) void k_prompt_join(PromptArgs a)
             A.y += w * v[i].y;
         }
     }
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    const float inv = M == kNegInf ? 0.0f : 1.0f / L;   // (no part with a key that the row sees: zero)
     *reinterpret_cast<vec2 *>(static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 2 * lane) = (vec2){(T)(A.x * inv), (T)(A.y * inv)};
 }
 

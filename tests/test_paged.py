@@ -7,6 +7,7 @@ Tolerance of an element y = sum p v / sum p over n tokens, with A = sum p |v| / 
   2 (n/4 + 300) 2^-24 A  sums in binary32: a wavefront adds every fourth 16 tokens, then states and parts are joined;
                          numerator and denominator"""
 import ctypes
+import math
 
 import pytest
 import torch
@@ -180,6 +181,33 @@ def test_decode_beyond_32_bit_offsets():
     near(out[0], q[0], k, v, t)
     from test_prompt import near as near_prompt
     near_prompt(out2, q, k, v, n - 1, t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("guide", [0, 20000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decode_scores_of_minus_infinity_and_nan(dtype, guide):
+    """A token whose score is -infinity has no weight, wherever it lies among the wavefronts and the parts; a sequence of them alone
+    is 0 / 0; a key that is NaN makes its sequence NaN, where it is the only one of its tile too."""
+    t, code = TYPES[dtype]
+    Hq, Hkv, P, keys = 4, 2, 32, [3000, 17, 500, 40, 65, 2000]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 33)
+    q = values((len(keys), Hq, D), t, 1)
+    q[:, :, 0] = 1.0
+    first = [2900, 16, 100, 40, 0, 1]        # tokens of weight 0, from the first on
+    for i, n in enumerate(first):
+        for j in range(n):
+            Kp[table[i + 1, j // P], :, j % P, 0] = -math.inf
+    Kp[table[5, 64 // P], :, 64 % P, 3] = math.nan     # the last token of the sequence of 65
+    Kp[table[6, 1999 // P], :, 1999 % P, 3] = math.nan
+    lens, rows = torch.tensor([7] + keys + [7], dtype=torch.int32).cuda(), torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    out = torch.full((len(keys), Hq, D), CANARY, device="cuda")
+    ds.ds_paged_decode(q.cuda(), Kp, Vp, out, rows, lens, table, ds.ds_paged_workspace_alloc(pg, len(keys), Hq, guide), pg, len(keys), Hq, guide)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[3:]).all()
+    for i in range(3):
+        near(out[i], q[i], kv[i][0][first[i]:], kv[i][1][first[i]:], t)
 
 
 # ------------------------------------------------------------------ append

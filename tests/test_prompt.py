@@ -360,3 +360,67 @@ def test_extreme_weights():
                                ds.ds_prompt_workspace_alloc(prm), prm)
         torch.cuda.synchronize()
         near(out, q, K, V, 560, t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("guide", [0, 60000])
+@pytest.mark.parametrize("form", ["packed", "paged"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_what_is_not_seen_is_not_finite(dtype, form, guide):
+    """Values and keys that are infinite or NaN touch the rows that see them, and there the channels that they are in:
+    not the rows before them, which share their tiles, nor other heads or sequences."""
+    t, code = TYPES[dtype]
+    Hq, Hkv, P, new, before = 6, 2, 16, [150, 20], [0, 300]
+    keys = [a + b for a, b in zip(new, before)]
+    qs, q = starts(new), values((sum(new), Hq, D), t, 1)
+    kv = [values((2, n, Hkv, D), t, 40 + i) for i, n in enumerate(keys)]
+    broken = [x.clone() for x in kv]
+    broken[0][1, 100, 0, 5], broken[0][1, 120, 0, 7] = math.inf, -math.inf     # values of KV head 0: rows 100.., 120..
+    broken[0][1, 149, 1, :] = math.nan                                         # of head 1: the last row alone
+    broken[1][0, 310, 1, 9] = math.nan                                         # a key of head 1, of the other sequence
+    prm = ds.prompt(2, Hq, Hkv, D, sum(new), guide, code, kv_elems=sum(keys) * Hkv * D)
+    ws = ds.ds_prompt_workspace_alloc(prm)
+    assert (ws.numel() > 256) == (guide > 0)
+    out = torch.full((sum(new), Hq, D), CANARY, dtype=t, device="cuda")
+    if form == "packed":
+        K, V = (torch.cat([x[i] for x in broken]).cuda() for i in (0, 1))
+        ds.ds_prompt_attention(q.cuda(), K, V, out, qs.cuda(), starts(keys)[:-1].contiguous().cuda(),
+                               torch.tensor(keys, dtype=torch.int32).cuda(), ws, prm)
+    else:
+        Kp, Vp, table, _ = paged(keys, Hkv, P, t, 20)
+        for i, x in enumerate(broken):
+            for j in range(keys[i]):
+                p = int(table[i + 1, j // P])
+                Kp[p, :, j % P], Vp[p, :, j % P] = x[0, j].cuda(), x[1, j].cuda()
+        pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+        ds.ds_prompt_attention_paged(q.cuda(), Kp, Vp, out, qs.cuda(), torch.tensor([1, 2], dtype=torch.int32).cuda(),
+                                     torch.tensor([0] + keys + [0], dtype=torch.int32).cuda(), table, ws, prm, pg)
+    torch.cuda.synchronize()
+    got, G = out.cpu(), Hq // Hkv
+    touched = torch.zeros(got.shape, dtype=torch.bool)
+    touched[100:150, :G, 5] = touched[120:150, :G, 7] = touched[149, G:] = touched[160:, G:] = True
+    assert not torch.isfinite(got[touched]).any()
+    for i, (m, b) in enumerate(zip(new, before)):
+        o = slice(int(qs[i]), int(qs[i + 1]))
+        y, A, e = defined(q[o], kv[i][0], kv[i][1], b)
+        # (a channel of a row that sees an infinity elsewhere: as if the infinity were any number there)
+        tol = torch.finfo(t).eps / 2 * (A + y.abs()) + 2 * e * A + 1e-7
+        assert ((got[o].double() - y).abs() <= tol)[~touched[o]].all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("guide", [0, 60000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scores_of_minus_infinity(dtype, guide):
+    """A key whose score is -infinity has no weight; a row of them alone is 0 / 0."""
+    t, code = TYPES[dtype]
+    q, K, V = values((200, 2, D), t, 1), values((200, 1, D), t, 2), values((200, 1, D), t, 3)
+    q[:, :, 0] = 1.0
+    K[:70, :, 0] = -math.inf
+    prm = ds.prompt(1, 2, 1, D, 200, guide, code, kv_elems=K.numel())
+    ws, zero, n = ds.ds_prompt_workspace_alloc(prm), torch.zeros(1, dtype=torch.int32).cuda(), torch.tensor([200], dtype=torch.int32).cuda()
+    out = torch.zeros_like(q).cuda()
+    ds.ds_prompt_attention(q.cuda(), K.cuda(), V.cuda(), out, starts([200]).cuda(), zero, n, ws, prm)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[:70]).all()
+    near(out[70:], q[70:], K[70:], V[70:], 0, t)
