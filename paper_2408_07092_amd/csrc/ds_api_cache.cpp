@@ -35,8 +35,8 @@ static bool prompt_ok(const ds_prompt_t *prm, ds_prompt_t *m)
         if (s % 8 != 0) return false;
     if (m->q_stride < row || m->out_stride < row || m->kv_stride < kD || m->kv_head_stride < kD || m->kv_elems < 0) return false;
     if (m->q_stride > most || m->out_stride > most || m->kv_stride > 1ll << 24 || m->kv_head_stride > 1ll << 40) return false;
-    // (a launch holds 2^32 threads at most, and rows are numbered in 32 bits)
-    return ((int64_t)m->total_q / kPromptRows + m->n_seqs) * m->Hq <= 1ll << 24;
+    // (a launch holds less than 2^32 threads, and rows are numbered in 32 bits)
+    return ((int64_t)m->total_q / kPromptRows + m->n_seqs) * m->Hq < 1ll << 24;
 }
 
 static bool pages_ok(const ds_pages_t *p)
@@ -194,7 +194,7 @@ ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages,
     const int64_t row = (int64_t)pages->Hkv * kD;
     if (new_stride == 0) new_stride = row;
     if (new_stride < row || new_stride % 8 != 0 || new_stride > 1ll << 30) return DS_ERR_SHAPE;
-    if ((int64_t)total_new * ((pages->Hkv + 7) / 8) > 1ll << 26) return DS_ERR_SHAPE;
+    if ((int64_t)total_new * ((pages->Hkv + 7) / 8) >= 1ll << 26) return DS_ERR_SHAPE;
     if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(K_pages, 256) || !aligned(V_pages, 256) ||
         !aligned(new_start, 4) || !aligned(rows, 4) || !aligned(start, 4) || !aligned(table, 4))
         return DS_ERR_ALIGN;
