@@ -188,6 +188,13 @@ def _stream(stream=None):
     return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
+def _stream_of(t, where: str, stream=None):
+    """The stream of a call whose tensors are where `t` is, which has to be the current device."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: a tensor is on {t.device}, which is not the current device")
+    return _stream(stream)
+
+
 def ds_version() -> int:
     return lib().ds_version()
 
@@ -397,7 +404,7 @@ def ds_prompt_workspace_alloc(prm: DsPrompt, device="cuda") -> "torch.Tensor":
 def ds_prompt_attention(q, K, V, out, q_start, kv_start, kv_len, workspace, prm: DsPrompt, stream=None):
     """q, K, V and out may be views with the strides that `prm` names."""
     _check(lib().ds_prompt_attention(_vp(q), _vp(K), _vp(V), _vp(out), _dp(q_start), _dp(kv_start), _dp(kv_len),
-                                     _dp(workspace), _bytes(workspace), ctypes.byref(prm), _stream(stream)),
+                                     _dp(workspace), _bytes(workspace), ctypes.byref(prm), _stream_of(q, "ds_prompt_attention", stream)),
            "ds_prompt_attention")
 
 
@@ -405,7 +412,7 @@ def ds_prompt_attention_paged(q, K_pages, V_pages, out, q_start, rows, lens, tab
                               pages: DsPages, stream=None):
     _check(lib().ds_prompt_attention_paged(_vp(q), _dp(K_pages), _dp(V_pages), _vp(out), _dp(q_start), _dp(rows),
                                            _dp(lens), _dp(table), _dp(workspace), _bytes(workspace),
-                                           ctypes.byref(prm), ctypes.byref(pages), _stream(stream)),
+                                           ctypes.byref(prm), ctypes.byref(pages), _stream_of(q, "ds_prompt_attention_paged", stream)),
            "ds_prompt_attention_paged")
 
 
@@ -422,7 +429,7 @@ def ds_paged_decode(q, K_pages, V_pages, out, rows, lens, table, workspace, page
                     max_len: int, stream=None):
     _check(lib().ds_paged_decode(_dp(q), _dp(K_pages), _dp(V_pages), _dp(out), _dp(rows), _dp(lens), _dp(table),
                                  _dp(workspace), _bytes(workspace), ctypes.byref(pages), n_seqs, Hq, max_len,
-                                 _stream(stream)), "ds_paged_decode")
+                                 _stream_of(q, "ds_paged_decode", stream)), "ds_paged_decode")
 
 
 def ds_append_paged(k_new, v_new, K_pages, V_pages, new_start, rows, start, table, pages: DsPages, n_seqs: int,
@@ -431,22 +438,22 @@ def ds_append_paged(k_new, v_new, K_pages, V_pages, new_start, rows, start, tabl
     assert k_new.shape[0] == v_new.shape[0] and k_new.stride() == v_new.stride() and k_new.stride()[1:] == (pages.d, 1)
     _check(lib().ds_append_paged(_vp(k_new), _vp(v_new), _dp(K_pages), _dp(V_pages), _dp(new_start), _dp(rows),
                                  _dp(start), _dp(table), ctypes.byref(pages), n_seqs, k_new.shape[0], k_new.stride(0),
-                                 _stream(stream)), "ds_append_paged")
+                                 _stream_of(k_new, "ds_append_paged", stream)), "ds_append_paged")
 
 
 def ds_pages_extend(refs, table, lens, rows, n_new, start, status, pages: DsPages, n: int, stream=None):
     _check(lib().ds_pages_extend(_dp(refs), _dp(table), _dp(lens), _dp(rows), _dp(n_new), _dp(start), _dp(status),
-                                 ctypes.byref(pages), n, _stream(stream)), "ds_pages_extend")
+                                 ctypes.byref(pages), n, _stream_of(refs, "ds_pages_extend", stream)), "ds_pages_extend")
 
 
 def ds_pages_fork(refs, table, lens, src, dst, copies, n_copies, status, pages: DsPages, n: int, stream=None):
     _check(lib().ds_pages_fork(_dp(refs), _dp(table), _dp(lens), _dp(src), _dp(dst), _dp(copies), _dp(n_copies),
-                               _dp(status), ctypes.byref(pages), n, _stream(stream)), "ds_pages_fork")
+                               _dp(status), ctypes.byref(pages), n, _stream_of(refs, "ds_pages_fork", stream)), "ds_pages_fork")
 
 
 def ds_pages_free(refs, table, lens, rows, status, pages: DsPages, n: int, stream=None):
     _check(lib().ds_pages_free(_dp(refs), _dp(table), _dp(lens), _dp(rows), _dp(status), ctypes.byref(pages), n,
-                               _stream(stream)), "ds_pages_free")
+                               _stream_of(refs, "ds_pages_free", stream)), "ds_pages_free")
 
 
 def ds_pages_workspace_bytes(pages: DsPages) -> int:
@@ -460,10 +467,10 @@ def ds_pages_workspace_alloc(pages: DsPages, device="cuda") -> "torch.Tensor":
 
 def ds_pages_compact(refs, table, lens, copies, n_copies, status, workspace, pages: DsPages, stream=None):
     _check(lib().ds_pages_compact(_dp(refs), _dp(table), _dp(lens), _dp(copies), _dp(n_copies), _dp(status),
-                                  _dp(workspace), _bytes(workspace), ctypes.byref(pages), _stream(stream)),
+                                  _dp(workspace), _bytes(workspace), ctypes.byref(pages), _stream_of(refs, "ds_pages_compact", stream)),
            "ds_pages_compact")
 
 
 def ds_pages_copy(K_pages, V_pages, copies, n_copies, pages: DsPages, max_copies: int, stream=None):
     _check(lib().ds_pages_copy(_dp(K_pages), _dp(V_pages), _dp(copies), _dp(n_copies), ctypes.byref(pages), max_copies,
-                               _stream(stream)), "ds_pages_copy")
+                               _stream_of(K_pages, "ds_pages_copy", stream)), "ds_pages_copy")

@@ -168,6 +168,18 @@ class Device:
         assert self.refs.tolist() == b.refs and self.lens.tolist() == b.lens and self.table.tolist() == b.table
 
 
+def test_tensors_off_the_device_are_refused():
+    """Memory of the host, which a kernel could not read, does not get as far as a launch."""
+    x, i, pg, prm = torch.zeros(1, 1, D), torch.zeros(4, dtype=torch.int32), ds.pages(1, 16, 1, D, 1, 1), ds.prompt(1, 1, 1, D, 1, 1)
+    for call in (lambda: ds.ds_prompt_attention(x, x, x, x, i, i, i, x, prm), lambda: ds.ds_prompt_attention_paged(x, x, x, x, i, i, i, i, x, prm, pg),
+                 lambda: ds.ds_paged_decode(x, x, x, x, i, i, i, x, pg, 1, 1, 1), lambda: ds.ds_append_paged(x, x, x, x, i, i, i, i, pg, 1),
+                 lambda: ds.ds_pages_extend(i, i, i, i, i, i, i, pg, 1), lambda: ds.ds_pages_fork(i, i, i, i, i, i, i, i, pg, 1),
+                 lambda: ds.ds_pages_free(i, i, i, i, i, pg, 1), lambda: ds.ds_pages_compact(i, i, i, i, i, i, x, pg),
+                 lambda: ds.ds_pages_copy(x, x, i, i, pg, 1)):
+        with pytest.raises(ValueError, match="not the current device"):
+            call()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n_pages,P,n_rows,max_pages", [(1, 16, 3, 2), (40, 16, 12, 7), (900, 32, 30, 60), (17000, 16, 70, 700), (40000, 256, 40, 1500)])
 def test_books_against_the_model(n_pages, P, n_rows, max_pages):
