@@ -374,8 +374,8 @@ typedef struct {
     int32_t dtype, reserved;              /* ds_dtype_t of the pools; 0                                  */
 } ds_pages_t;
 
-/* Bytes of workspace that a prompt call needs (a multiple of 256; cleared once with ds_workspace_init like
- * every workspace).  Pure host function; 0 if the shape is invalid. */
+/* Bytes of workspace that a prompt call needs (a multiple of 256).  It need not be cleared, and serves every
+ * call that it is large enough for.  Pure host function; 0 if the shape is invalid. */
 size_t ds_prompt_workspace_bytes(const ds_prompt_t *prm);
 ds_status_t ds_prompt_attention(const void *q, const void *K, const void *V, void *out,
                                 const int32_t *q_start, const int32_t *kv_start, const int32_t *kv_len,
@@ -394,6 +394,8 @@ ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const 
  * zeros; one whose row, length or pages cannot be gives NaN, and nothing is read outside the table and the pools.
  * Pools 256-byte aligned, q, out and workspace 16-byte.  n_seqs, Hq < 1, bad heads, rows NULL with n_seqs > n_rows,
  * or n_seqs * Hkv * ceil(G / 16) * (ceil(max_pages * page_tokens / 64) + 3) beyond 2^31 -> DS_ERR_SHAPE.
+ * The workspace is cleared once (ds_workspace_init); it then serves every call of the same Hq and Hkv, of any n_seqs,
+ * max_len and pages, that it is large enough for (n_seqs and Hq, Hkv make its size, the lengths do not).
  */
 size_t ds_paged_workspace_bytes(const ds_pages_t *pages, int32_t n_seqs, int32_t Hq, int32_t max_len);
 ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pages, float *out,

@@ -165,8 +165,8 @@ ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pa
     a.K = K_pages;
     a.V = V_pages;
     a.out = out;
-    a.arrived = static_cast<uint32_t *>(workspace);
-    a.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.off_part);
+    a.part = static_cast<float *>(workspace);
+    a.arrived = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + p.off_arrived);
     a.rows = rows;
     a.lens = lens;
     a.table = table;

@@ -82,7 +82,7 @@ struct PagedArgs {
 struct PagedPlan {
     int G, passes, GH, least, wgs;
     bool join_here;
-    size_t off_part, total;
+    size_t off_arrived, total;
 };
 void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan *p);
 hipError_t launch_paged(PagedArgs a, const PagedPlan &p, int dtype, hipStream_t st);

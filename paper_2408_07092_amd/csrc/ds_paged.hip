@@ -446,8 +446,10 @@ void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan 
     // Up to eight parts a unit the last workgroup joins for all heads (32 units of 900 tokens 10.8 us, with a launch of its own
     // for the join 11.9); more are joined by a workgroup for each head (4 units of 250K tokens, 64 parts: 119 -> 110).
     p->join_here = p->wgs <= 8 * units;
-    p->off_part = ((size_t)units * 4 + 255) / 256 * 256;
-    p->total = (p->off_part + (size_t)p->wgs * 2 * p->GH * kPartStride * 4 + 255) / 256 * 256;
+    // Parts first, room for as many as there can be: the counters, which are zero between calls, are then never where calls
+    // of other sequences have parts, and one workspace serves all of them.
+    p->off_arrived = (size_t)device_caps().cus * 2 * p->GH * kPartStride * 4;
+    p->total = (p->off_arrived + (size_t)units * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_paged(PagedArgs a, const PagedPlan &p, int dtype, hipStream_t st)

@@ -210,6 +210,26 @@ def test_decode_scores_of_minus_infinity_and_nan(dtype, guide):
         near(out[i], q[i], kv[i][0][first[i]:], kv[i][1][first[i]:], t)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(2, 2), (24, 2)], ids=str)
+def test_decode_workspace_serves_other_batches(heads):
+    """One workspace, cleared once, for more and fewer sequences in turn: what one call leaves of its parts is not where
+    another counts its workgroups."""
+    t, code, P, (Hq, Hkv) = torch.float16, ds.DS_F16, 32, heads
+    keys = [3000, 5, 9000, 64, 65] + [100 + 7 * i for i in range(60)]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 34)
+    q = values((len(keys), Hq, D), t, 1).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    ws = ds.ds_paged_workspace_alloc(pg, len(keys), Hq, 0)
+    lens, rows = torch.tensor([7] + keys + [7], dtype=torch.int32).cuda(), torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda()
+    for n, guide in ((1, 3000), (65, 9000), (3, 9000), (65, 0), (2, 100000), (30, 9000), (65, 9000)):
+        out = torch.full((n, Hq, D), CANARY, device="cuda")
+        ds.ds_paged_decode(q[:n], Kp, Vp, out, rows[:n], lens, table, ws, pg, n, Hq, guide)
+        torch.cuda.synchronize()
+        for i in range(n):
+            near(out[i], q[i], kv[i][0], kv[i][1], t)
+
+
 # ------------------------------------------------------------------ append
 @pytest.mark.gpu
 @pytest.mark.parametrize("Hkv", [1, 3, 8, 40])
