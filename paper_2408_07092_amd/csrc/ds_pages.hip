@@ -154,16 +154,18 @@ __global__ __launch_bounds__(kBooks) void k_pages_extend(PagesArgs a)
     if (tid == 0) *a.status = (int32_t)code;
 }
 
-// dst shares src's full pages: wavefront w of n_waves takes every n_waves-th entry of the list.
-__device__ __forceinline__ void share_pages(const PagesArgs &a, int w, int n_waves)
+// dst shares src's full pages: wavefront (w, y) of n_waves by n_y takes every n_waves-th entry of the list, and every
+// n_y-th 256 pages of it.
+constexpr int kShared = 256;
+__device__ __forceinline__ void share_pages(const PagesArgs &a, int w, int n_waves, int y, int n_y)
 {
-    constexpr int kFlight = 4;
+    constexpr int kFlight = kShared / 64;
     const int lane = threadIdx.x & 63;
     for (int i = w; i < a.n; i += n_waves) {
         const int32_t *from = a.table + (size_t)a.rows[i] * a.max_pages;
         int32_t *to = a.table + (size_t)a.dst[i] * a.max_pages;
         const int full = a.lens[a.rows[i]] >> a.page_log2;
-        for (int j0 = lane; j0 < full; j0 += 64 * kFlight) {
+        for (int j0 = y * kShared + lane; j0 < full; j0 += n_y * kShared) {
             int p[kFlight];
 #pragma unroll
             for (int k = 0; k < kFlight; ++k) p[k] = from[min(j0 + 64 * k, full - 1)];
@@ -221,7 +223,8 @@ __global__ __launch_bounds__(kBooks) void k_pages_fork(PagesArgs a, int share)
     __syncthreads();
     if (!code) {
         // (lens of the branches come last: share_pages reads those of the sources, which are other rows)
-        if (share) share_pages(a, tid >> 6, kBookWaves);
+        const int wave = tid >> 6, n_y = max(1, kBookWaves / a.n);
+        if (share) share_pages(a, wave / n_y, kBookWaves / n_y, wave % n_y, n_y);
 #pragma unroll
         for (int k = 0; k < kListed; ++k)
             if (tid * kListed + k < a.n) {
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(kBooks) void k_pages_fork(PagesArgs a, int share)
 }
 __global__ __launch_bounds__(kWG) void k_pages_share(PagesArgs a)
 {
-    if (*a.status == 0) share_pages(a, (int)(blockIdx.x * (kWG / 64) + (threadIdx.x >> 6)), (int)(gridDim.x * (kWG / 64)));
+    if (*a.status == 0) share_pages(a, (int)blockIdx.x, (int)gridDim.x, (int)(blockIdx.y * (kWG / 64) + (threadIdx.x >> 6)), (int)(gridDim.y * (kWG / 64)));
 }
 
 // Rows end: see ds_pages_free.  A workgroup for each row; each looks at the whole list, so that all agree on it.
@@ -262,10 +265,17 @@ __global__ __launch_bounds__(kWG) void k_pages_free(PagesArgs a)
     const int row = a.rows[blockIdx.x];
     const int held = min(pages_in(a, a.lens[row]), a.max_pages);
     int32_t *entry = a.table + (size_t)row * a.max_pages;
-    for (int j = tid; j < held; j += kWG) {
-        const int p = entry[j];
-        if ((uint32_t)p < (uint32_t)a.n_pages) atomicSub(&a.refs[p], 1);
-        entry[j] = -1;
+    constexpr int kFlight = 8;
+    for (int j0 = tid; j0 < held; j0 += kWG * kFlight) {
+        int p[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) p[k] = entry[min(j0 + kWG * k, held - 1)];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k)
+            if (j0 + kWG * k < held) {
+                if ((uint32_t)p[k] < (uint32_t)a.n_pages) atomicSub(&a.refs[p[k]], 1);
+                entry[j0 + kWG * k] = -1;
+            }
     }
     __syncthreads();
     if (tid == 0) a.lens[row] = 0;
@@ -360,10 +370,14 @@ hipError_t launch_pages_extend(const PagesArgs &a, hipStream_t st)
 
 hipError_t launch_pages_fork(const PagesArgs &a, hipStream_t st)
 {
-    // One workgroup shares up to 16 rows of 256 entries in one step; more than a few of these are worth a launch.
-    const bool alone = (int64_t)a.n * a.max_pages <= 16384;
+    // The workgroup that keeps the books shares the full pages too if each of its wavefronts has 256 of them at most; more are
+    // worth a launch.  (us of a fork and the freeing of its branches, one launch and two: one row of 256 pages 6.6 and 7.7,
+    // 16 of 256 9.0 and 10.0, 4 of 512 8.7 and 9.4; on the other side 32 of 64 9.3 and 9.0, 16 of 1024 13.9 and 10.8,
+    // 256 of 64 25 and 9.5.)
+    const int n_y = std::max(1, kBookWaves / a.n), per = (a.max_pages + kShared - 1) / kShared;
+    const bool alone = a.n <= kBookWaves && per <= n_y;
     DS_LAUNCH(KID_PAGES_FORK, k_pages_fork, dim3(1), dim3(kBooks), 0, st, a, alone ? 1 : 0);
-    if (!alone) DS_LAUNCH(KID_PAGES_FORK, k_pages_share, dim3((a.n + kWG / 64 - 1) / (kWG / 64)), dim3(kWG), 0, st, a);
+    if (!alone) DS_LAUNCH(KID_PAGES_FORK, k_pages_share, dim3(a.n, std::min((per + kWG / 64 - 1) / (kWG / 64), 64)), dim3(kWG), 0, st, a);
     return hipGetLastError();
 }
 
