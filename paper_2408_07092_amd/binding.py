@@ -163,9 +163,20 @@ def _dp(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
+# (The calls of the paged cache are small, and a step makes many: they pass addresses as plain integers, which costs
+#  a third of a ctypes object.)
+def _at(t):
+    """Address of a contiguous tensor, or NULL."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return t.data_ptr()
+
+
 def _vp(t):
-    """Pointer of a tensor whose strides the call is told of, or NULL."""
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    """Address of a tensor whose strides the call is told of, or NULL."""
+    return None if t is None else t.data_ptr()
 
 
 def _bytes(t) -> int:
@@ -190,9 +201,10 @@ def _stream(stream=None):
 
 def _stream_of(t, where: str, stream=None):
     """The stream of a call whose tensors are where `t` is, which has to be the current device."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+    device = t.get_device()   # (-1: memory of the host)
+    if device < 0 or device != torch._C._cuda_getDevice():
         raise ValueError(f"{where}: a tensor is on {t.device}, which is not the current device")
-    return _stream(stream)
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def ds_version() -> int:
@@ -403,15 +415,15 @@ def ds_prompt_workspace_alloc(prm: DsPrompt, device="cuda") -> "torch.Tensor":
 
 def ds_prompt_attention(q, K, V, out, q_start, kv_start, kv_len, workspace, prm: DsPrompt, stream=None):
     """q, K, V and out may be views with the strides that `prm` names."""
-    _check(lib().ds_prompt_attention(_vp(q), _vp(K), _vp(V), _vp(out), _dp(q_start), _dp(kv_start), _dp(kv_len),
-                                     _dp(workspace), _bytes(workspace), ctypes.byref(prm), _stream_of(q, "ds_prompt_attention", stream)),
+    _check(lib().ds_prompt_attention(_vp(q), _vp(K), _vp(V), _vp(out), _at(q_start), _at(kv_start), _at(kv_len),
+                                     _at(workspace), _bytes(workspace), ctypes.byref(prm), _stream_of(q, "ds_prompt_attention", stream)),
            "ds_prompt_attention")
 
 
 def ds_prompt_attention_paged(q, K_pages, V_pages, out, q_start, rows, lens, table, workspace, prm: DsPrompt,
                               pages: DsPages, stream=None):
-    _check(lib().ds_prompt_attention_paged(_vp(q), _dp(K_pages), _dp(V_pages), _vp(out), _dp(q_start), _dp(rows),
-                                           _dp(lens), _dp(table), _dp(workspace), _bytes(workspace),
+    _check(lib().ds_prompt_attention_paged(_vp(q), _at(K_pages), _at(V_pages), _vp(out), _at(q_start), _at(rows),
+                                           _at(lens), _at(table), _at(workspace), _bytes(workspace),
                                            ctypes.byref(prm), ctypes.byref(pages), _stream_of(q, "ds_prompt_attention_paged", stream)),
            "ds_prompt_attention_paged")
 
@@ -427,8 +439,8 @@ def ds_paged_workspace_alloc(pages: DsPages, n_seqs: int, Hq: int, max_len: int,
 
 def ds_paged_decode(q, K_pages, V_pages, out, rows, lens, table, workspace, pages: DsPages, n_seqs: int, Hq: int,
                     max_len: int, stream=None):
-    _check(lib().ds_paged_decode(_dp(q), _dp(K_pages), _dp(V_pages), _dp(out), _dp(rows), _dp(lens), _dp(table),
-                                 _dp(workspace), _bytes(workspace), ctypes.byref(pages), n_seqs, Hq, max_len,
+    _check(lib().ds_paged_decode(_at(q), _at(K_pages), _at(V_pages), _at(out), _at(rows), _at(lens), _at(table),
+                                 _at(workspace), _bytes(workspace), ctypes.byref(pages), n_seqs, Hq, max_len,
                                  _stream_of(q, "ds_paged_decode", stream)), "ds_paged_decode")
 
 
@@ -436,23 +448,23 @@ def ds_append_paged(k_new, v_new, K_pages, V_pages, new_start, rows, start, tabl
                     stream=None):
     """k_new, v_new [total_new, Hkv, d], dense or views that step the same from token to token."""
     assert k_new.shape[0] == v_new.shape[0] and k_new.stride() == v_new.stride() and k_new.stride()[1:] == (pages.d, 1)
-    _check(lib().ds_append_paged(_vp(k_new), _vp(v_new), _dp(K_pages), _dp(V_pages), _dp(new_start), _dp(rows),
-                                 _dp(start), _dp(table), ctypes.byref(pages), n_seqs, k_new.shape[0], k_new.stride(0),
+    _check(lib().ds_append_paged(_vp(k_new), _vp(v_new), _at(K_pages), _at(V_pages), _at(new_start), _at(rows),
+                                 _at(start), _at(table), ctypes.byref(pages), n_seqs, k_new.shape[0], k_new.stride(0),
                                  _stream_of(k_new, "ds_append_paged", stream)), "ds_append_paged")
 
 
 def ds_pages_extend(refs, table, lens, rows, n_new, start, status, pages: DsPages, n: int, stream=None):
-    _check(lib().ds_pages_extend(_dp(refs), _dp(table), _dp(lens), _dp(rows), _dp(n_new), _dp(start), _dp(status),
+    _check(lib().ds_pages_extend(_at(refs), _at(table), _at(lens), _at(rows), _at(n_new), _at(start), _at(status),
                                  ctypes.byref(pages), n, _stream_of(refs, "ds_pages_extend", stream)), "ds_pages_extend")
 
 
 def ds_pages_fork(refs, table, lens, src, dst, copies, n_copies, status, pages: DsPages, n: int, stream=None):
-    _check(lib().ds_pages_fork(_dp(refs), _dp(table), _dp(lens), _dp(src), _dp(dst), _dp(copies), _dp(n_copies),
-                               _dp(status), ctypes.byref(pages), n, _stream_of(refs, "ds_pages_fork", stream)), "ds_pages_fork")
+    _check(lib().ds_pages_fork(_at(refs), _at(table), _at(lens), _at(src), _at(dst), _at(copies), _at(n_copies),
+                               _at(status), ctypes.byref(pages), n, _stream_of(refs, "ds_pages_fork", stream)), "ds_pages_fork")
 
 
 def ds_pages_free(refs, table, lens, rows, status, pages: DsPages, n: int, stream=None):
-    _check(lib().ds_pages_free(_dp(refs), _dp(table), _dp(lens), _dp(rows), _dp(status), ctypes.byref(pages), n,
+    _check(lib().ds_pages_free(_at(refs), _at(table), _at(lens), _at(rows), _at(status), ctypes.byref(pages), n,
                                _stream_of(refs, "ds_pages_free", stream)), "ds_pages_free")
 
 
@@ -466,11 +478,11 @@ def ds_pages_workspace_alloc(pages: DsPages, device="cuda") -> "torch.Tensor":
 
 
 def ds_pages_compact(refs, table, lens, copies, n_copies, status, workspace, pages: DsPages, stream=None):
-    _check(lib().ds_pages_compact(_dp(refs), _dp(table), _dp(lens), _dp(copies), _dp(n_copies), _dp(status),
-                                  _dp(workspace), _bytes(workspace), ctypes.byref(pages), _stream_of(refs, "ds_pages_compact", stream)),
+    _check(lib().ds_pages_compact(_at(refs), _at(table), _at(lens), _at(copies), _at(n_copies), _at(status),
+                                  _at(workspace), _bytes(workspace), ctypes.byref(pages), _stream_of(refs, "ds_pages_compact", stream)),
            "ds_pages_compact")
 
 
 def ds_pages_copy(K_pages, V_pages, copies, n_copies, pages: DsPages, max_copies: int, stream=None):
-    _check(lib().ds_pages_copy(_dp(K_pages), _dp(V_pages), _dp(copies), _dp(n_copies), ctypes.byref(pages), max_copies,
+    _check(lib().ds_pages_copy(_at(K_pages), _at(V_pages), _at(copies), _at(n_copies), ctypes.byref(pages), max_copies,
                                _stream_of(K_pages, "ds_pages_copy", stream)), "ds_pages_copy")
