@@ -35,7 +35,7 @@ struct PromptArgs {
     int64_t q_stride, out_stride, kv_stride, kv_head_stride, kv_elems;
     float2 *part_ml;                              // [n_split][total_q][Hq]: maximum and sum of a row over a part of the keys
     float *part_acc;                              // [n_split][total_q][Hq][d]: its numerator
-    int n_seqs, Hq, Hkv, G, total_q, n_tiles, n_split;
+    int n_seqs, Hq, Hkv, G, total_q, n_tiles, n_split, cus;
     int n_pages, page_log2, max_pages, n_table;   // paged only
 };
 struct PromptPlan {
@@ -43,7 +43,7 @@ struct PromptPlan {
     size_t off_acc, total;
 };
 bool make_prompt_plan(const ds_prompt_t &m, PromptPlan *p);
-hipError_t launch_prompt(const PromptArgs &a, bool paged, int dtype, hipStream_t st);
+hipError_t launch_prompt(PromptArgs a, bool paged, int dtype, hipStream_t st);
 
 // Row tiles of packed sequences, numbered without a prefix sum: sequence s has its tiles from number
 // floor(q_start[s] G / 128) + s on, which leaves room for the part tile that each one may end in.

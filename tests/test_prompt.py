@@ -424,3 +424,23 @@ def test_scores_of_minus_infinity(dtype, guide):
     torch.cuda.synchronize()
     assert torch.isnan(out[:70]).all()
     near(out[70:], q[70:], K[70:], V[70:], 0, t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(64, 64), (96, 32)], ids=str)
+def test_more_workgroups_than_compute_units_but_not_twice_as_many(heads):
+    """Every row tile of every head has its workgroup where they are dealt out by weight."""
+    t, code, (Hq, Hkv), new = torch.bfloat16, ds.DS_BF16, heads, [300, 220]
+    tiles = sum(new) * (Hq // Hkv) // 128 + len(new)
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    assert cus < tiles * Hkv <= 2 * cus
+    T, qs = sum(new), starts(new)
+    q, K, V = values((T, Hq, D), t, 1).cuda(), values((T, Hkv, D), t, 2, True).cuda(), values((T, Hkv, D), t, 3).cuda()
+    prm = ds.prompt(2, Hq, Hkv, D, T, max(new), code, kv_elems=K.numel())
+    out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+    ds.ds_prompt_attention(q, K, V, out, qs.cuda(), qs[:-1].contiguous().cuda(), torch.tensor(new, dtype=torch.int32).cuda(),
+                           ds.ds_prompt_workspace_alloc(prm), prm)
+    torch.cuda.synchronize()
+    for i in range(2):
+        r = slice(int(qs[i]), int(qs[i + 1]))
+        near(out[r], q[r], K[r], V[r], 0, t)
