@@ -69,6 +69,7 @@ __device__ __forceinline__ int last_at_or_before(int n, int x, Key key)
 // ---------------------------------------------------------------- paged decode
 constexpr int kPiece = 64;         // tokens that a share is counted in: 16 for each wavefront of a workgroup
 constexpr int kLead = 3;           // pieces that a unit counts for besides its own
+constexpr int kWhole = 4;          // a unit of up to so many pieces is not cut
 
 struct PagedArgs {
     const void *q, *K, *V;

@@ -4,7 +4,8 @@
 // The attention reads every K and V row once and computes next to nothing on it: memory bound.  Lengths are
 // known on the device only and may differ as they like, so the work is cut there: all the
 // sequences' tokens, a KV head after the other, are one line of pieces of 64 tokens, of which every workgroup
-// takes an equal, contiguous share.  A share covers the end of one unit (sequence and KV head), whole units, and
+// takes an equal, contiguous share, but for units of up to kWhole pieces, which are not cut (an end that falls into one
+// moves to its nearer end: 101 sequences of up to 89 tokens, 2 groups of 16 13.8 -> 7.0 us).  A share covers the end of one unit (sequence and KV head), whole units, and
 // the beginning of another, or a part of a single one; a unit's parts meet in the workspace, where
 // the last workgroup to arrive joins them in their order along the cache.  Which part holds
 // which tokens follows from the lengths and the launch alone, so results do not depend on who is last.
@@ -14,7 +15,8 @@
 // workgroups 405, 318 and 347; with two tiles and two workgroups 332; one sequence of 250K (512 MB) 89, and 118 to
 // 182 with one tile and two to four workgroups, whose parts cost more to join.  A unit's beginning and end (its query, the
 // wavefronts' states, the part) cost a workgroup about what three pieces do, and count as kLead pieces: 48 sequences of 3 to 20000
-// tokens 157 us without, 109, 102 and 100 with one, two and three.
+// tokens 157 us without, 109, 102 and 100 with one, two and three (since then, with a head's states combined by a
+// wavefront, 91 and the writing of the new rows 5).
 //
 // A wavefront takes 16 tokens at a time (within one page, as pages hold 16 or more), for up to 16 heads
 // of the group at once:
@@ -146,6 +148,43 @@ __device__ __forceinline__ void join_parts(const PagedArgs &a, int w0, int w1, i
     }
 }
 
+// Combines the wavefronts' states (maximum, sum, two of padding, numerator) to a unit's part, or to its rows of the
+// output: a wavefront for a head, two channels a lane.  All threads call it.
+template <int GH>
+__device__ __forceinline__ void combine_states(const float (*wpart)[GH][kPartStride], int n_heads, float *part, float *out)
+{
+    const int lane = threadIdx.x & 63;
+    __syncthreads();
+#pragma unroll
+    for (int g0 = 0; g0 < GH; g0 += 4) {
+        const int g = g0 + (int)(threadIdx.x >> 6);
+        if (g >= n_heads) break;
+        float2 ml[4], v[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            ml[w] = *reinterpret_cast<const float2 *>(&wpart[w][g][0]);
+            v[w] = *reinterpret_cast<const float2 *>(&wpart[w][g][4 + 2 * lane]);
+        }
+        const float M = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+        float L = 0.0f;
+        float2 A = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(ml[w].x - M);
+            L += f * ml[w].y;
+            A.x += f * v[w].x;
+            A.y += f * v[w].y;
+        }
+        if (out) {
+            *reinterpret_cast<float2 *>(out + (size_t)g * kD + 2 * lane) = make_float2(A.x / L, A.y / L);
+        } else {
+            uint2 *pg = reinterpret_cast<uint2 *>(part + (size_t)g * kPartStride);
+            st_dev(pg + 2 + lane, make_uint2(__float_as_uint(A.x), __float_as_uint(A.y)));
+            if (lane == 0) st_dev(pg, make_uint2(__float_as_uint(M), __float_as_uint(L)));
+        }
+    }
+}
+
 // All pieces of the call's sequences, and those ahead of sequence `upto` (threads of a workgroup each take some).
 __device__ __forceinline__ void count_pieces(const PagedArgs &a, int upto, uint32_t *s_w, uint32_t *total, uint32_t *before)
 {
@@ -169,12 +208,12 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
     typedef typename Mma16<T>::vec4 vec4;
     __shared__ __attribute__((aligned(16))) float wpart[4][GH][kPartStride];
     __shared__ __attribute__((aligned(16))) float sc_sh[4][16];
-    __shared__ uint32_t s_w[4], s_flag, s_at[4];
+    __shared__ uint32_t s_w[4], s_flag, s_at[2][4];
     float (*red)[kD + 4] = reinterpret_cast<float (*)[kD + 4]>(&wpart[0][0][0]);   // (4 of them; used after wpart)
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lo = lane & 15, hi = lane >> 4;
     const int units = a.Hkv * a.passes;   // of a sequence
-    // ---- all pieces, and where this workgroup's share starts
+    // ---- all pieces
     const int per = (a.n + kWG - 1) / kWG;
     uint32_t mine = 0;
     int n = 1, row = 0;
@@ -199,23 +238,36 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
     const uint32_t W = shares_of(a, T_all, gridDim.x);
     if (blockIdx.x >= W || T_all == 0) return;
     const Shares shares(T_all, W);
-    uint32_t x = shares.start(blockIdx.x);
-    const uint32_t x_end = shares.start(blockIdx.x + 1);
-    const uint32_t want = x / (uint32_t)units;     // the piece of a sequence that the share starts in, counted over sequences
-    if (ahead <= want && want < ahead + mine) {
-        int b = tid * per;
-        if (per > 1)
-            for (uint32_t k; (k = (uint32_t)pieces_of(n = row_tokens(a, b, &row))) <= want - ahead; ++b) ahead += k;
-        s_at[0] = (uint32_t)b;
-        s_at[1] = ahead;
-        s_at[2] = (uint32_t)n;
-        s_at[3] = (uint32_t)row;
+    // ---- the sequences that the share's ends lie in
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t want = shares.start(blockIdx.x + e) / (uint32_t)units;   // the piece of a sequence, counted over sequences
+        if (ahead <= want && want < ahead + mine) {
+            int b = tid * per;
+            uint32_t at = ahead;
+            if (per > 1)
+                for (uint32_t k; (k = (uint32_t)pieces_of(n = row_tokens(a, b, &row))) <= want - at; ++b) at += k;
+            s_at[e][0] = (uint32_t)b;
+            s_at[e][1] = at;
+            s_at[e][2] = (uint32_t)n;
+            s_at[e][3] = (uint32_t)row;
+        }
     }
     __syncthreads();
-    int b = __builtin_amdgcn_readfirstlane((int)s_at[0]);
-    uint32_t seq0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_at[1]) * (uint32_t)units;       // first piece of sequence b
-    n = __builtin_amdgcn_readfirstlane((int)s_at[2]);
-    row = __builtin_amdgcn_readfirstlane((int)s_at[3]);
+    // (an end within a short unit moves to the nearer end of it)
+    auto end_of = [&](int e) {
+        const uint32_t x = shares.start(blockIdx.x + e);
+        if (x >= T_all) return T_all;
+        const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_at[e][1]) * (uint32_t)units;
+        const uint32_t np = (uint32_t)pieces_of(__builtin_amdgcn_readfirstlane((int)s_at[e][2])), r = (x - first) % np;
+        return np > kWhole + kLead ? x : 2 * r < np ? x - r : x - r + np;
+    };
+    uint32_t x = end_of(0);
+    const uint32_t x_end = end_of(1);
+    int b = __builtin_amdgcn_readfirstlane((int)s_at[0][0]);
+    uint32_t seq0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_at[0][1]) * (uint32_t)units;       // first piece of sequence b
+    n = __builtin_amdgcn_readfirstlane((int)s_at[0][2]);
+    row = __builtin_amdgcn_readfirstlane((int)s_at[0][3]);
 
     while (x < x_end) {
         const uint32_t np = (uint32_t)pieces_of(n);
@@ -356,20 +408,18 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
             m = 0.0f;
             l = __builtin_nanf("");
         }
-        if (hi == 0 && lo < n_heads) {
-            wpart[wave][lo][0] = m;
-            wpart[wave][lo][1] = l;
-        }
+        if (hi == 0 && lo < n_heads) *reinterpret_cast<float2 *>(&wpart[wave][lo][0]) = make_float2(m, l);
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr)
             if (4 * hi + rr < n_heads) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) wpart[wave][4 * hi + rr][4 + 8 * lo + e] = O[e][rr];
+                for (int e = 0; e < 8; e += 4)
+                    *reinterpret_cast<f32x4 *>(&wpart[wave][4 * hi + rr][4 + 8 * lo + e]) = (f32x4){O[e][rr], O[e + 1][rr], O[e + 2][rr], O[e + 3][rr]};
             }
         const bool whole = p0 == 0 && p1 == (int)np - kLead;
         // (a share has at most one part of a unit that an earlier share began, and one of a unit that goes on)
         float *po = a.part + ((size_t)blockIdx.x * 2 + (p0 == 0 ? 1 : 0)) * GH * kPartStride;
-        wg_combine_store<GH>(wpart, n_heads, po, kPartStride, whole ? a.out + head0 * kD : nullptr);
+        combine_states<GH>(wpart, n_heads, po, whole ? a.out + head0 * kD : nullptr);
         if (!whole && a.join_here) {
             const int w0 = (int)shares.of(unit0 + kLead), w1 = (int)shares.of(unit0 + np - 1);
             uint32_t *arrived = a.arrived + (size_t)b * units + u;
@@ -394,7 +444,7 @@ __global__ __launch_bounds__(kWG) void k_paged_join(PagedArgs a, uint32_t wgs)
     count_pieces(a, b, s_w, &total, &ahead);
     int row;
     const uint32_t np = (uint32_t)pieces_of(row_tokens(a, b, &row)), T_all = total * (uint32_t)units;
-    if (np == 0) return;
+    if (np <= kWhole + kLead) return;
     const Shares shares(T_all, shares_of(a, T_all, wgs));
     const int h = hq / a.G, g = hq % a.G;
     const uint32_t unit0 = ahead * (uint32_t)units + (uint32_t)(h * a.passes + g / 16) * np;
@@ -442,13 +492,18 @@ void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan 
     // Shares of no less than two pieces (one sequence of 900 tokens, 32 heads: 10.8 us, of four 11.7, of eight 14.0).
     p->least = 2;
     const int64_t units = (int64_t)n * g.Hkv * p->passes, pieces = units * std::max(1, (max_len + kPiece - 1) / kPiece);
-    p->wgs = (int)std::min<int64_t>(pieces, device_caps().cus);
+    // One workgroup to a compute unit reads fastest.  Where units are many and short it waits for one's lengths, page and rows after
+    // the other's, and a second one is worth its bandwidth: 65 sequences of up to 24 tokens, 40 heads 25.5 us with one and 15.9 with two,
+    // 32 of up to 200, 32 heads 26.8 and 25.1; on the other side 128 of up to 500, 8 groups of 8 50.2 and 52.5, one of 900, 32
+    // heads 11.1 and 14.3.
+    const int cus = device_caps().cus, at_once = pieces <= kWhole * units && units >= 4 * cus ? 2 : 1;
+    p->wgs = (int)std::min<int64_t>(pieces, at_once * cus);
     // Up to eight parts a unit the last workgroup joins for all heads (32 units of 900 tokens 10.8 us, with a launch of its own
     // for the join 11.9); more are joined by a workgroup for each head (4 units of 250K tokens, 64 parts: 119 -> 110).
     p->join_here = p->wgs <= 8 * units;
     // Parts first, room for as many as there can be: the counters, which are zero between calls, are then never where calls
     // of other sequences have parts, and one workspace serves all of them.
-    p->off_arrived = (size_t)device_caps().cus * 2 * p->GH * kPartStride * 4;
+    p->off_arrived = (size_t)2 * cus * 2 * p->GH * kPartStride * 4;
     p->total = (p->off_arrived + (size_t)units * 4 + 255) / 256 * 256;
 }
 

@@ -230,6 +230,30 @@ def test_decode_workspace_serves_other_batches(heads):
             near(out[i], q[i], kv[i][0], kv[i][1], t)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(8, 8), (32, 2)], ids=str)
+@pytest.mark.parametrize("n", [1, 4, 40])
+def test_decode_short_beside_long(n, heads):
+    """Units that are not cut (up to 256 tokens) between units that are, wherever the shares' ends fall; the guide, and with it
+    the number of shares, from one to all that there are."""
+    t, code, P, (Hq, Hkv) = torch.bfloat16, ds.DS_BF16, 16, heads
+    keys = ([5, 3000, 257, 256, 20, 5000, 64, 320, 321, 1, 700, 0, 255, 1500] * 3)[:n]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 35)
+    q = values((n, Hq, D), t, 1).cuda()
+    lens, rows = torch.tensor([7] + keys + [7], dtype=torch.int32).cuda(), torch.arange(1, n + 1, dtype=torch.int32).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    ws = ds.ds_paged_workspace_alloc(pg, n, Hq, 0)
+    for guide in (0, 64, 200, 1000, 100000):
+        out = torch.full((n, Hq, D), CANARY, device="cuda")
+        ds.ds_paged_decode(q, Kp, Vp, out, rows, lens, table, ws, pg, n, Hq, guide)
+        torch.cuda.synchronize()
+        for i in range(n):
+            if keys[i]:
+                near(out[i], q[i], kv[i][0], kv[i][1], t)
+            else:
+                assert (out[i] == 0).all()
+
+
 # ------------------------------------------------------------------ append
 @pytest.mark.gpu
 @pytest.mark.parametrize("Hkv", [1, 3, 8, 40])
