@@ -6,15 +6,15 @@
 // over the keys j <= i + nk - nq, in one pass over the keys with a running maximum m and a
 // running sum.  Bound by the matrix units: 4 d flops a pair against a few bytes for each row.  8K tokens of 32 heads take
 // 528 us (1.04 PFLOP/s), two of 8K in groups of 4 986 us; a library product of 16384 x 16384 x 16384 reaches 1.3 to 1.37.  What
-// holds it there is power: the same launch on zeros takes 352 us, and on random data the clock is at 1.68 GHz, with the
-// matrix units busy in 58 % of the cycles.  Short prompts are bound by a workgroup's steps one after the other, 1.2 us each
+// holds it there is power: the same launch on zeros takes 352 us, and on random data the clock is at 1.6 to 1.7 GHz, with
+// the matrix units busy in 58 % of the cycles.  Short prompts are bound by a workgroup's steps one after the other, 1.2 us each
 // with the compute unit to itself (97 tokens 7.5 us, 500 in groups of 4 15.8, 1500 of 32 heads 39).
 //
 // The G query heads of a KV head are rows of one matrix: row token * G + g.  A workgroup takes 128 of
 // these rows, a wavefront 32, and walks the keys in tiles of 64 that all of its wavefronts share from LDS.  Two
 // workgroups share a compute unit, 64 KiB and 240 registers a lane each.  (Two of 8K tokens in groups of 4, before the
 // loads went between the products: 1081 us; with eight wavefronts to a workgroup and three tiles on their way 1102; with 64 rows to a wavefront, which
-// halves the reads of LDS but leaves its registers too few, 1394.  Eight wavefronts of which four take each half of the keys: 1500
+// halves the reads of LDS but leaves one wavefront to a SIMD, 1394, and at best, long after, 1096 beside 1031.  Eight wavefronts of which four take each half of the keys: 1500
 // tokens 42 -> 37, but packed prompts 63 -> 76 and 8K tokens 527 -> 560.)
 // Everything is computed transposed, so that a query row is a column and lives in one lane (and the
 // lane 32 away, which has the other half of the keys): its maximum, sum and rescaling are
