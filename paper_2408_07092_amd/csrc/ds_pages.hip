@@ -22,7 +22,7 @@ __device__ __forceinline__ bool length_ok(const PagesArgs &a, int64_t tokens) { 
 struct BooksLds {
     uint32_t seen[65536 / 32];        // a bit for every row
     uint32_t w[kBookWaves];
-    uint32_t bad, got;
+    uint32_t bad;
 };
 
 // Marks row r; whether it was marked already or is none.

@@ -425,3 +425,46 @@ def test_streams_and_repeats():
     torch.cuda.synchronize()
     for o, p in outs[1:]:
         assert torch.equal(o, outs[0][0]) and torch.equal(p.view(torch.int16), outs[0][1].view(torch.int16))
+
+
+@pytest.mark.gpu
+def test_two_captured_calls_share_a_workspace():
+    """Decode and split prompts of two batches, captured apart with one workspace each for both, replayed in turn with eager calls of
+    a third batch between: every time the bits of the eager calls."""
+    t, code, P, Hq, Hkv, keys = torch.float16, ds.DS_F16, 16, 8, 2, [3000, 40, 0, 700, 5001]
+    from test_prompt import paged, starts
+    Kp, Vp, table, _ = paged(keys, Hkv, P, t, 41)
+    table, lens = table[1:-1].contiguous(), ints(keys)
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, len(keys), table.shape[1], code)
+    calls = []
+    for rows, new in (([4, 0, 3], [1, 9, 30]), ([0, 1, 2, 3, 4], [5, 2, 0, 1, 16]), ([1, 4], [20, 3])):
+        n, T = len(rows), sum(new)
+        calls.append(dict(n=n, rows=ints(rows), q=values((n, Hq, D), t, n).cuda(), qp=values((T, Hq, D), t, 10 + n).cuda(), qs=starts(new).cuda(),
+                          prm=ds.prompt(n, Hq, Hkv, D, T, 5001, code), o=torch.zeros((n, Hq, D), device="cuda"),
+                          p=torch.zeros((T, Hq, D), dtype=t, device="cuda")))
+    ws = ds.ds_paged_workspace_alloc(pg, 5, Hq, 5001)
+    wp = torch.empty(max(ds.ds_prompt_workspace_bytes(c["prm"]) for c in calls), dtype=torch.uint8, device="cuda")
+    assert wp.numel() > 256
+
+    def run(c):
+        ds.ds_paged_decode(c["q"], Kp, Vp, c["o"], c["rows"], lens, table, ws, pg, c["n"], Hq, 5001)
+        ds.ds_prompt_attention_paged(c["qp"], Kp, Vp, c["p"], c["qs"], c["rows"], lens, table, wp, c["prm"], pg)
+
+    for c in calls:
+        run(c)
+    torch.cuda.synchronize()
+    want = [(c["o"].clone(), c["p"].clone()) for c in calls]
+    graphs = []
+    for c in calls[:2]:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(c)
+        graphs.append(g)
+    for i in range(6):
+        for j in ((0, 2, 1) if i % 2 else (1, 0, 2)):
+            c = calls[j]
+            c["o"].fill_(7.0)
+            c["p"].fill_(7.0)
+            graphs[j].replay() if j < 2 else run(c)
+            torch.cuda.synchronize()
+            assert torch.equal(c["o"], want[j][0]) and torch.equal(c["p"], want[j][1]), (i, j)
