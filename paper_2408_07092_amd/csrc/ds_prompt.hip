@@ -438,16 +438,23 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         } else {
             // (a row whose pages or places are not there is NaN, one that sees no key is zero)
             const float inv = bad ? __builtin_nanf("") : my_last < 0 ? 0.0f : 1.0f / l;
-            T *dst = static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 4 * hi;
+            T *dst = static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 8 * hi;
+            // (four channels of a lane and the next four of the lane 32 away, exchanged for whole pieces of 16 bytes: 97 tokens of 32
+            // heads 8.0 -> 7.4 us, 12 of 300 in groups of 4 32.4 -> 28.4, 8 of 2407 in pairs 443 -> 431.  Whole rows by way of LDS: no better.)
             typedef T vec4 __attribute__((ext_vector_type(4)));
+            auto four = [&](int d, int i) {
+                vec4 x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = (T)(O[d][4 * i + j] * inv);
+                return __builtin_bit_cast(u32x2, x);
+            };
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    vec4 x;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] = (T)(O[d][4 * i + j] * inv);
-                    *reinterpret_cast<vec4 *>(dst + d * 32 + i * 8) = x;
+                for (int i = 0; i < 4; i += 2) {
+                    const u32x2 x = four(d, i), y = four(d, i + 1);
+                    const u32x2 u = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false), v = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+                    *reinterpret_cast<u32x4 *>(dst + d * 32 + i * 8) = (u32x4){u.x, v.x, u.y, v.y};
                 }
         }
     }
