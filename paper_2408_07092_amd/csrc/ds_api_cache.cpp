@@ -174,7 +174,6 @@ ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pa
     a.Hkv = pages->Hkv;
     a.G = p.G;
     a.passes = p.passes;
-    a.least = p.least;
     a.join_here = p.join_here;
     a.n_pages = pages->n_pages;
     a.page_log2 = log2_of(pages->page_tokens);

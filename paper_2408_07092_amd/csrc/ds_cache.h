@@ -23,6 +23,22 @@ constexpr int kMostTokens = 1 << 30;  // of a sequence: what the kernels step pa
 // away (2^(kLeast - m) = 0), and the weights of scores of -infinity are 0, not 2^(-inf + inf).
 constexpr float kLeast = -3e38f;
 
+// n / d of 0 <= n < 2^31 by a product: with 2^(l-1) < d <= 2^l and m = floor(2^(31+l) / d) + 1, m d lies between 2^(31+l) and
+// 2^(31+l) + 2^l, so n m / 2^(31+l) exceeds n / d by less than 1 / d.  (A division of the compiler's is a chain of some 25
+// instructions, and a workgroup's beginning had ten of them.)
+struct Quotient {
+    uint32_t m;
+    int shift;
+    void set(uint32_t d)
+    {
+        int l = 0;
+        while ((1ull << l) < d) ++l;
+        m = (uint32_t)((1ull << (31 + l)) / d + 1);
+        shift = 31 + l;
+    }
+    __device__ __forceinline__ int of(int n) const { return (int)((uint64_t)(uint32_t)n * m >> shift); }
+};
+
 // ---------------------------------------------------------------- prompt attention
 constexpr int kPromptRows = 128;   // rows (token * G + head of the group) of a workgroup
 constexpr int kPromptParts = 64;   // parts that keys are split into at most: a lane of the join for each
@@ -35,6 +51,7 @@ struct PromptArgs {
     int64_t q_stride, out_stride, kv_stride, kv_head_stride, kv_elems;
     float2 *part_ml;                              // [n_split][total_q][Hq]: maximum and sum of a row over a part of the keys
     float *part_acc;                              // [n_split][total_q][Hq][d]: its numerator
+    Quotient by_G, by_Hkv, by_Hq;
     int n_seqs, Hq, Hkv, G, total_q, n_tiles, n_split, cus;
     int n_pages, page_log2, max_pages, n_table;   // paged only
 };
@@ -70,18 +87,20 @@ __device__ __forceinline__ int last_at_or_before(int n, int x, Key key)
 constexpr int kPiece = 64;         // tokens that a share is counted in: 16 for each wavefront of a workgroup
 constexpr int kLead = 3;           // pieces that a unit counts for besides its own
 constexpr int kWhole = 4;          // a unit of up to so many pieces is not cut
+constexpr int kShareAtLeast = 2;   // pieces
 
 struct PagedArgs {
     const void *q, *K, *V;
     float *out, *part;
     uint32_t *arrived;             // per sequence and unit, zero between calls
     const int32_t *rows, *lens, *table;
-    int n, Hkv, G, passes, least;  // passes of 16 heads over a KV head's rows; least pieces of a share
+    Quotient by_units, by_passes;
+    int n, Hkv, G, passes;         // passes of 16 heads over a KV head's rows
     bool join_here;                // parts are joined by the workgroup that is last, not by a launch after this one
     int n_pages, page_log2, max_pages, n_table;
 };
 struct PagedPlan {
-    int G, passes, GH, least, wgs;
+    int G, passes, GH, wgs;
     bool join_here;
     size_t off_arrived, total;
 };

@@ -198,7 +198,8 @@ __device__ __forceinline__ void count_pieces(const PagedArgs &a, int upto, uint3
     block_exclusive_scan(all, s_w, total);
     block_exclusive_scan(ahead, s_w, before);
 }
-__device__ __forceinline__ uint32_t shares_of(const PagedArgs &a, uint32_t T_all, uint32_t wgs) { return max(1u, min(wgs, T_all / (uint32_t)a.least)); }
+// (one sequence of 900 tokens, 32 heads, in shares of no less than two pieces 10.8 us, of four 11.7, of eight 14.0)
+__device__ __forceinline__ uint32_t shares_of(uint32_t T_all, uint32_t wgs) { return max(1u, min(wgs, T_all / kShareAtLeast)); }
 
 template <class T, int GH>
 __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
@@ -235,13 +236,13 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
     uint32_t total;
     uint32_t ahead = block_exclusive_scan(mine, s_w, &total);
     const uint32_t T_all = total * (uint32_t)units;
-    const uint32_t W = shares_of(a, T_all, gridDim.x);
+    const uint32_t W = shares_of(T_all, gridDim.x);
     if (blockIdx.x >= W || T_all == 0) return;
     const Shares shares(T_all, W);
     // ---- the sequences that the share's ends lie in
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const uint32_t want = shares.start(blockIdx.x + e) / (uint32_t)units;   // the piece of a sequence, counted over sequences
+        const uint32_t want = (uint32_t)a.by_units.of((int)shares.start(blockIdx.x + e));   // the piece of a sequence, counted over sequences
         if (ahead <= want && want < ahead + mine) {
             int b = tid * per;
             uint32_t at = ahead;
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
             n = row_tokens(a, ++b, &row);
             continue;
         }
-        const int u = (int)((x - seq0) / np), h = u / a.passes, g0 = (u % a.passes) * 16;
+        const int u = (int)((x - seq0) / np), h = a.by_passes.of(u), g0 = (u - h * a.passes) * 16;
         const uint32_t unit0 = seq0 + (uint32_t)u * np;
         // (a share that ends within a unit's lead leaves it to the next)
         const int p0 = max((int)(x - unit0) - kLead, 0), p1 = (int)min(np, x_end - unit0) - kLead;
@@ -445,7 +446,7 @@ __global__ __launch_bounds__(kWG) void k_paged_join(PagedArgs a, uint32_t wgs)
     int row;
     const uint32_t np = (uint32_t)pieces_of(row_tokens(a, b, &row)), T_all = total * (uint32_t)units;
     if (np <= kWhole + kLead) return;
-    const Shares shares(T_all, shares_of(a, T_all, wgs));
+    const Shares shares(T_all, shares_of(T_all, wgs));
     const int h = hq / a.G, g = hq % a.G;
     const uint32_t unit0 = ahead * (uint32_t)units + (uint32_t)(h * a.passes + g / 16) * np;
     const int w0 = (int)shares.of(unit0 + kLead), w1 = (int)shares.of(unit0 + np - 1);
@@ -489,8 +490,6 @@ void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan 
     p->G = Hq / g.Hkv;
     p->passes = (p->G + 15) / 16;
     p->GH = p->G <= 4 ? 4 : p->G <= 8 ? 8 : 16;
-    // Shares of no less than two pieces (one sequence of 900 tokens, 32 heads: 10.8 us, of four 11.7, of eight 14.0).
-    p->least = 2;
     const int64_t units = (int64_t)n * g.Hkv * p->passes, pieces = units * std::max(1, (max_len + kPiece - 1) / kPiece);
     // One workgroup to a compute unit reads fastest.  Where units are many and short it waits for one's lengths, page and rows after
     // the other's, and a second one is worth its bandwidth: 65 sequences of up to 24 tokens, 40 heads 25.5 us with one and 15.9 with two,
@@ -509,6 +508,8 @@ void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan 
 
 hipError_t launch_paged(PagedArgs a, const PagedPlan &p, int dtype, hipStream_t st)
 {
+    a.by_units.set((uint32_t)(a.Hkv * a.passes));
+    a.by_passes.set((uint32_t)a.passes);
     const bool bf = dtype == DS_BF16;
     void (*fn)(PagedArgs) = p.GH == 4   ? (bf ? k_paged<__bf16, 4> : k_paged<_Float16, 4>)
                             : p.GH == 8 ? (bf ? k_paged<__bf16, 8> : k_paged<_Float16, 8>)

@@ -148,11 +148,12 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     int rank = blockIdx.x;
     const int W = gridDim.x, twice = W - a.cus;
     if (twice > 0 && twice <= a.cus) rank = rank < twice ? a.cus - twice + rank : rank < a.cus ? rank - twice : W - 1 - (rank - a.cus);
-    const int kvh = rank % a.Hkv;
-    const int slot = a.n_tiles - 1 - rank / a.Hkv;
+    const int kvh = rank - a.by_Hkv.of(rank) * a.Hkv;
+    const int slot = a.n_tiles - 1 - a.by_Hkv.of(rank);
     // ---- the sequence and its rows
     const int s = last_at_or_before(a.n_seqs, slot, [&](int i) { return tile_base(a.q_start[i], a.G, i); });
     const int qs = a.q_start[s], qe = a.q_start[s + 1];
+    const int word0 = PAGED ? (a.rows ? a.rows[s] : s) : a.kv_start[s], word1 = PAGED ? 0 : a.kv_len[s];   // (with these, not after them)
     if (qs < 0 || qe < qs || qe > a.total_q) return;
     const int n_rows = (qe - qs) * a.G;
     const int r0 = (slot - tile_base(qs, a.G, s)) * kPromptRows;
@@ -162,22 +163,22 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     int64_t kv0 = 0;
     const int32_t *pages = nullptr;
     if constexpr (PAGED) {
-        const int row = a.rows ? a.rows[s] : s;
+        const int row = word0;
         bad = row < 0 || row >= a.n_table;
         nk = bad ? 0 : a.kv_len[row];
         pages = a.table + (size_t)(bad ? 0 : row) * a.max_pages;
         bad |= nk < 0 || (int64_t)nk > (int64_t)a.max_pages << a.page_log2;
     } else {
-        nk = a.kv_len[s];
-        kv0 = a.kv_start[s];
+        nk = word1;
+        kv0 = word0;
         bad = nk < 0 || nk > kMostTokens || kv0 < 0 || (nk > 0 && (kv0 + nk - 1) * a.kv_stride + (int64_t)(a.Hkv - 1) * a.kv_head_stride + kD > a.kv_elems);
         kv0 = kv0 * a.kv_stride + (int64_t)kvh * a.kv_head_stride;
     }
     if (bad) nk = 0;
     const int last_row = min(n_rows, r0 + kPromptRows) - 1;
-    const int seen = max(0, min(nk, last_row / a.G + nk - (qe - qs) + 1));    // keys that some row of the workgroup sees
+    const int seen = max(0, min(nk, a.by_G.of(last_row) + nk - (qe - qs) + 1));    // keys that some row of the workgroup sees
     // ---- its part of them, where the keys are split; from here on keys count from its first
-    const int all_kt = (seen + kKeys - 1) / kKeys, part_kt = (all_kt + a.n_split - 1) / a.n_split;
+    const int all_kt = (seen + kKeys - 1) / kKeys, part_kt = a.n_split == 1 ? all_kt : (all_kt + a.n_split - 1) / a.n_split;
     const int kt0 = min((int)blockIdx.y * part_kt, all_kt), n_kt = min(part_kt, all_kt - kt0);
     const int first_key = kt0 * kKeys;
     const int before = nk - (qe - qs) - first_key;   // keys ahead of the sequence's first row's own
@@ -185,15 +186,15 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     if constexpr (!PAGED) kv0 += first_key * a.kv_stride;
     const int my_row = r0 + wave * 32 + lo;
     const bool on = my_row < n_rows;
-    const int my_last = on ? min(my_row / a.G + before, nk - 1) : -1; // last key that the lane's row sees
+    const int my_last = on ? min(a.by_G.of(my_row) + before, nk - 1) : -1; // last key that the lane's row sees
     // tiles that some row of the wavefront sees, and those that all of its rows see whole
-    const int n_mine = min(n_kt, max(0, (min(r0 + wave * 32 + 31, n_rows - 1)) / a.G + before + kKeys) / kKeys);
-    const int n_clear = r0 + wave * 32 >= n_rows ? 0 : max(0, min((r0 + wave * 32) / a.G + before + 1, nk)) / kKeys;
+    const int n_mine = min(n_kt, max(0, a.by_G.of(min(r0 + wave * 32 + 31, n_rows - 1)) + before + kKeys) / kKeys);
+    const int n_clear = r0 + wave * 32 >= n_rows ? 0 : max(0, min(a.by_G.of(r0 + wave * 32) + before + 1, nk)) / kKeys;
 
     vec8 q[8];
     {
-        const int row = min(my_row, n_rows - 1);
-        const T *src = static_cast<const T *>(a.q) + (size_t)(qs + row / a.G) * a.q_stride + (size_t)(kvh * a.G + row % a.G) * kD + hi * 8;
+        const int row = min(my_row, n_rows - 1), own = a.by_G.of(row);
+        const T *src = static_cast<const T *>(a.q) + (size_t)(qs + own) * a.q_stride + (size_t)(kvh * a.G + row - own * a.G) * kD + hi * 8;
 #pragma unroll
         for (int x = 0; x < 8; ++x) q[x] = *reinterpret_cast<const vec8 *>(src + x * 16);
     }
@@ -421,8 +422,8 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     }
     if (on) {
         l = halves_sum(l);
-        const int64_t token = qs + my_row / a.G;
-        const int head = kvh * a.G + my_row % a.G;
+        const int own = a.by_G.of(my_row), head = kvh * a.G + my_row - own * a.G;
+        const int64_t token = qs + own;
         if (a.n_split > 1) {
             const int64_t row = ((int64_t)blockIdx.y * a.total_q + token) * a.Hq + head;
             if (my_last < 0) m = kNegInf;                // (a part without a key that the row sees)
@@ -470,8 +471,8 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     const uint32_t anew = (uint32_t)beyond | (uint32_t)(beyond >> 32);
     if (anew) __threadfence();   // (they are written once more)
     for (uint32_t left = anew; left; left &= left - 1u) {
-        const int row = r0 + wave * 32 + __builtin_ctz(left), head = kvh * a.G + row % a.G;
-        const int64_t token = qs + row / a.G;
+        const int row = r0 + wave * 32 + __builtin_ctz(left), own = a.by_G.of(row), head = kvh * a.G + row - own * a.G;
+        const int64_t token = qs + own;
         auto at = [&](int j) -> int64_t {
             if constexpr (PAGED) {
                 const int t = first_key + j;
@@ -480,7 +481,7 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
                 return kv0 + j * a.kv_stride;
             }
         };
-        const int last = min(row / a.G + before, nk - 1);
+        const int last = min(own + before, nk - 1);
         float m1, l1;
         float2 A;
         row_alone(static_cast<const T *>(a.q) + token * a.q_stride + (int64_t)head * kD, static_cast<const T *>(a.K),
@@ -506,7 +507,7 @@ __global__ __launch_bounds__(kWG) void k_prompt_join(PromptArgs a)
     const int64_t rows = (int64_t)a.total_q * a.Hq;
     const int64_t row = (int64_t)blockIdx.x * (kWG / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (row >= rows) return;
-    const int token = (int)(row / a.Hq), head = (int)(row % a.Hq);
+    const int token = a.by_Hq.of((int)row), head = (int)row - token * a.Hq;
     const int s = last_at_or_before(a.n_seqs, token, [&](int i) { return a.q_start[i]; });
     const int qs = a.q_start[s], qe = a.q_start[s + 1];
     if (qs < 0 || qe < qs || qe > a.total_q || token < qs || token >= qe) return;   // (no row of a sequence: left as it is)
@@ -576,6 +577,9 @@ static PromptFn prompt_fn(bool paged, int dtype)
 hipError_t launch_prompt(PromptArgs a, bool paged, int dtype, hipStream_t st)
 {
     a.cus = device_caps().cus;
+    a.by_G.set(a.G);
+    a.by_Hkv.set(a.Hkv);
+    a.by_Hq.set(a.Hq);
     const PromptFn fn = prompt_fn(paged, dtype);
     DS_LAUNCH(KID_PROMPT, fn, dim3((unsigned)(a.n_tiles * a.Hkv), a.n_split), dim3(kWG), 4 * kTileBytes, st, a);
     if (a.n_split > 1) {
