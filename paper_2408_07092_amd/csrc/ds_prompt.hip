@@ -351,8 +351,11 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
     ids0 = page_ids(2);
     wait_tiles();
     f32x16 S0[2], S1[2];
+    if (n_mine > 0) scores(0, S0, [](int) {});
+    // (Every wavefront reads the first K tile here, and what comes next brings another to its place: in the loop the barrier
+    //  at the end of a step lies between the two.  Without further tiles nothing is brought.)
+    if (n_kt > 1) __syncthreads();
     if (n_mine > 0) {
-        scores(0, S0, [](int) {});
         if (n_clear < 1) hide(0, S0);
         raise(S0);
     }

@@ -444,3 +444,43 @@ def test_more_workgroups_than_compute_units_but_not_twice_as_many(heads):
     for i in range(2):
         r = slice(int(qs[i]), int(qs[i + 1]))
         near(out[r], q[r], K[r], V[r], 0, t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("guide", [0, 600])
+@pytest.mark.parametrize("form", ["packed", "paged"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_tiles_of_many_heads(dtype, form, guide):
+    """One to four tiles of keys, two workgroups to a compute unit, wavefronts of unlike work in a workgroup (down to one tile of
+    three): the first tile is whole until all of them have read it.  Again and again the same bits, the definition's."""
+    t, code, P = TYPES[dtype] + (16,)
+    Hq = Hkv = 96
+    new, before = [97, 128, 128, 100, 128, 65, 70], [0, 1, 32, 17, 60, 130, 0]
+    if guide:      # fewer rows, so that the keys are split; parts of up to three tiles
+        Hq = Hkv = 8
+        new, before = [97, 128, 70], [400, 501, 32]
+    keys = [a + b for a, b in zip(new, before)]
+    T, qs, ks = sum(new), starts(new), starts(keys)
+    q = values((T, Hq, D), t, 1).cuda()
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 50)
+    K, V = (torch.cat([x[i] for x in kv]).cuda() for i in (0, 1))
+    rows, lens = torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda(), torch.tensor([9] + keys + [9], dtype=torch.int32).cuda()
+    prm = ds.prompt(len(new), Hq, Hkv, D, T, guide, code, kv_elems=K.numel())
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    ws = ds.ds_prompt_workspace_alloc(prm)
+    assert (ws.numel() > 256) == (guide > 0)
+    args = qs.cuda(), ks[:-1].contiguous().cuda(), torch.tensor(keys, dtype=torch.int32).cuda()
+    first = None
+    for _ in range(30):
+        out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+        if form == "packed":
+            ds.ds_prompt_attention(q, K, V, out, *args, ws, prm)
+        else:
+            ds.ds_prompt_attention_paged(q, Kp, Vp, out, args[0], rows, lens, table, ws, prm, pg)
+        torch.cuda.synchronize()
+        if first is None:
+            first = out
+            for i, (m, b) in enumerate(zip(new, before)):
+                o = slice(int(qs[i]), int(qs[i + 1]))
+                near(out[o], q[o], kv[i][0], kv[i][1], b, t)
+        assert torch.equal(out, first)
