@@ -27,6 +27,7 @@
 // One head alone leaves 15 of 16 columns of the matrix units idle, which costs nothing here: 16 tokens take
 // about 500 clocks of one SIMD, and their 8 KiB about 700 of the compute unit's share of memory.
 #include <algorithm>
+#include <type_traits>
 
 #include "ds_device.h"
 #include "ds_cache.h"
@@ -293,6 +294,10 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
             q[i] = (vec8)(T)0;
             if (lo < n_heads) q[i] = *reinterpret_cast<const vec8 *>(static_cast<const T *>(a.q) + (head0 + lo) * kD + 8 * (4 * i + hi));
         }
+        // Weights are 2^(s - m + lead), which cancels in the quotient: in fp16 so that their low parts are normal numbers, in bf16, whose
+        // values reach as far as binary32's, so that the weights of all n tokens add up to 1 at most and no numerator, of a
+        // wavefront, a part or the whole, exceeds the largest value.
+        const float lead = std::is_same_v<T, __bf16> ? -(float)(n > 1 ? 32 - __builtin_clz(n - 1) : 0) : kPScaleLog2;
         float m = kLeast, l = 0.0f;
         f32x4 O[8];
 #pragma unroll
@@ -347,7 +352,7 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
             m = mn;
             float p[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - mn + kPScaleLog2);
+            for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[r] - mn + lead);
             l = l * sc + ((p[0] + p[1]) + (p[2] + p[3]));
             if (__any(sc != 1.0f)) {
                 if (hi == 0) sc_sh[wave][lo] = sc;
@@ -355,7 +360,7 @@ __global__ __launch_bounds__(kWG, 2) void k_paged(PagedArgs a)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) O[e] *= f;
             }
-            // a weight as the sum of two numbers of V's type: 22 bits in fp16 (the scale keeps the low part normal), 16 in bf16
+            // a weight as the sum of two numbers of V's type: 22 bits in fp16, 16 in bf16
             vec4 p_hi, p_lo;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {

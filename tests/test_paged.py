@@ -211,6 +211,32 @@ def test_decode_scores_of_minus_infinity_and_nan(dtype, guide):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("guide", [0, 20000])
+@pytest.mark.parametrize("size", [1e35, 3.3895e38, 1e-20])
+def test_decode_over_the_range_of_bf16(size, guide):
+    """Values as large as bf16 has, in one token and in all of them, in one part and in many: the result is a number, theirs."""
+    t, code, P, Hq, Hkv, keys = torch.bfloat16, ds.DS_BF16, 16, 8, 2, [1, 17, 64, 300, 3000, 20011]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 36)
+    for i, x in enumerate(kv):
+        v = x[1].float()
+        v = torch.where(torch.arange(D) % 3 == 0, torch.full_like(v, size), (v / v.abs().max() * size)).to(t)   # (equal ones add up)
+        assert torch.isfinite(v).all()
+        x[1] = v
+        for j in range((keys[i] + P - 1) // P):
+            part = v[j * P:(j + 1) * P].transpose(0, 1)
+            Vp[table[i + 1, j], :, :part.shape[1]] = part.cuda()
+    q = values((len(keys), Hq, D), t, 1)
+    q[:, 0] = 0.0                                  # (equal weights)
+    lens, rows = torch.tensor([7] + keys + [7], dtype=torch.int32).cuda(), torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    out = torch.full((len(keys), Hq, D), CANARY, device="cuda")
+    ds.ds_paged_decode(q.cuda(), Kp, Vp, out, rows, lens, table, ds.ds_paged_workspace_alloc(pg, len(keys), Hq, guide), pg, len(keys), Hq, guide)
+    torch.cuda.synchronize()
+    for i in range(len(keys)):
+        near(out[i] / size, q[i], kv[i][0], kv[i][1].double() / size, t)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("heads", [(2, 2), (24, 2)], ids=str)
 def test_decode_workspace_serves_other_batches(heads):
     """One workspace, cleared once, for more and fewer sequences in turn: what one call leaves of its parts is not where
