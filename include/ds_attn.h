@@ -344,7 +344,8 @@ ds_status_t ds_attend_rows(const void *q, const void *KV_rows, float *out,
  * within its row of the page table or on pages of the pool, or are more than 2^30, gets NaN, and nothing is
  * read outside.
  * Keys that a row does not see have no part in it, whatever they and their values hold, infinities and NaN
- * too; a row that sees such a value takes a slow path, a key at a time.
+ * too.  Rows that see such a value, or stand beside one in a tile, and rows whose sums overflow (bf16) are formed a second time,
+ * after which sums of finite values are finite; a call all of whose rows are takes some five times as long.
  * max_kv: keys of the longest sequence (a guide to the split, which the results do not rest on).
  */
 typedef enum { DS_F16 = 0, DS_BF16 = 1 } ds_dtype_t; /* IEEE binary16; bfloat16 */

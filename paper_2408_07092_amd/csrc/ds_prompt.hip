@@ -89,46 +89,106 @@ __device__ __forceinline__ void wait_tiles()
     __syncthreads();
 }
 
-// One row of a head anew, a key at a time, over its keys 0 .. last: at(j) is the element of key j's row.  The wavefront
-// takes 64 keys at once for the scores, a lane each, and two channels a lane for the values.  Weights are
-// 2^(s - m) here, so sums of finite values overflow only where the values themselves nearly do.
+// The V operand of a product: keys 16 c .., channels 32 d .. of rows that lie from vb on.  (The steps of k_prompt have it written out: called from
+// there, the compiler moves the reads from their places among the products, 500 tokens in groups of 4 14.5 -> 15.0 us.)
+template <class T>
+__device__ __forceinline__ typename Mma<T>::vec8 v_operand(const u32x4 *vb, int c, int d)
+{
+    const int lane = threadIdx.x & 63;
+    const int r = 16 * c + (lane >> 5) * 4 + (lane & 15) / 4, piece = d * 4 + ((lane >> 4) & 1) * 2 + (lane & 3) / 2;
+    const char *v0 = reinterpret_cast<const char *>(vb + v_piece(r, piece)) + (lane & 1) * 8;
+    const char *v1 = reinterpret_cast<const char *>(vb + v_piece(r + 8, piece)) + (lane & 1) * 8;
+    const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v0);
+    const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)v1);
+    const s16x8 v = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+    return __builtin_bit_cast(typename Mma<T>::vec8, v);
+}
+
+// A wavefront's 32 rows once more, by itself and 32 keys at a time, for those whose numerator is not finite: a value that is
+// not finite comes into rows of the same tile that do not see its key as well, 0 times it being NaN, and sums of
+// large bf16 values overflow.  last: the last key that some row sees; my_last: that the lane's row sees; all rows see the keys before
+// `clear`.  In tiles that hold others, values that are not finite are taken out of the products and added to the rows that
+// see them.  Weights are 2^(s - m + *room), in bf16 such that they add up to 1 at most: no numerator exceeds the largest
+// value.  lds: 8 KiB of the wavefront's own.
+// Nothing is on its way while it computes: where all rows come here a call takes five times as long (4096 tokens, 16 / 8 heads, a NaN in the
+// first value 90 -> 447 us, in all of them 495; the same in pages of 64 105 -> 484 and 534).
 template <class T, class At>
-__device__ __forceinline__ void row_alone(const T *q, const T *K, const T *V, int last, At at, float *m, float *l, float2 *A)
+__device__ __forceinline__ void rows_again(const T *q, const T *K, const T *V, int last, int my_last, int clear, At at, u32x4 *lds, float *room, float *m, float *l, f32x16 (&O)[4])
 {
     typedef typename Mma<T>::vec8 vec8;
-    typedef T vec2 __attribute__((ext_vector_type(2)));
-    const int lane = threadIdx.x & 63;
-    *m = last < 0 ? kNegInf : kLeast;
+    typedef T vec4 __attribute__((ext_vector_type(4)));
+    const int lane = threadIdx.x & 63, lo = lane & 31, hi = lane >> 5;
+    *room = std::is_same_v<T, __bf16> ? -(float)(last > 0 ? 32 - __builtin_clz(last) : 0) : kRoom;
+    *m = kLeast;
     *l = 0.0f;
-    *A = make_float2(0.0f, 0.0f);
-    for (int t0 = 0; t0 <= last; t0 += 64) {
-        const T *k = K + at(min(t0 + lane, last));
-        float s = 0.0f;
-#pragma unroll 1
-        for (int x = 0; x < kD; x += 8) {
-            const vec8 kx = *reinterpret_cast<const vec8 *>(k + x), qx = *reinterpret_cast<const vec8 *>(q + x);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s = __builtin_fmaf((float)kx[j], (float)qx[j], s);
+    for (int d = 0; d < 4; ++d) O[d] = (f32x16)(0.0f);
+    vec8 qx[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) qx[x] = *reinterpret_cast<const vec8 *>(q + x * 16 + hi * 8);
+#pragma unroll 1
+    for (int t0 = 0; t0 <= last; t0 += 32) {
+        const T *k = K + at(min(t0 + lo, last)) + hi * 8;
+        f32x16 S = (f32x16)(0.0f);
+        vec8 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const vec8 *>(V + at(min(t0 + 4 * i + (lane >> 4), last)) + (lane & 15) * 8);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) S = Mma<T>::dot(*reinterpret_cast<const vec8 *>(k + x * 16), qx[x], S);
+        uint32_t beyond = 0u;   // bit i: v[i] was not finite somewhere
+        if (t0 + 32 > clear) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (!(fabsf((float)v[i][j]) < __builtin_inff())) {
+                        v[i][j] = (T)0.0f;
+                        beyond |= 1u << i;
+                    }
         }
-        s = t0 + lane <= last ? s * kPromptScale : kNegInf;
-        float top = s;
+        __builtin_amdgcn_wave_barrier();   // (the reads of the tile before come first)
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-        top = fmaxf(top, *m);
-        const float f = __builtin_amdgcn_exp2f(*m - top), p = __builtin_amdgcn_exp2f(s - top);
-        float sum = p;
+        for (int i = 0; i < 8; ++i) lds[v_piece(4 * i + (lane >> 4), lane & 15)] = __builtin_bit_cast(u32x4, v[i]);
+        __builtin_amdgcn_wave_barrier();
+        float top = kNegInf;
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-        *m = top;
-        *l = *l * f + sum;
-        A->x *= f;
-        A->y *= f;
+        for (int i = 0; i < 16; ++i) {
+            if (t0 + 8 * (i / 4) + 4 * hi + i % 4 > my_last) S[i] = kNegInf;
+            top = fmaxf(top, S[i]);
+        }
+        const float mn = fmaxf(*m, halves_max(top) * kPromptScale), f = __builtin_amdgcn_exp2f(*m - mn), shift = *room - mn;
+        *m = mn;
+        *l *= f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) O[d] *= f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            vec8 P;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) P[j] = (T)__builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * c + j], kPromptScale, shift));   // (rounded as in the tiles' steps)
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) *l = Mma<T>::add2((typename Mma<T>::vec2){P[j], P[j + 1]}, *l);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) O[d] = Mma<T>::dot(v_operand<T>(lds, c, d), P, O[d]);
+        }
 #pragma unroll 1
-        for (int i = 0; i < min(64, last - t0 + 1); ++i) {
-            const vec2 v = *reinterpret_cast<const vec2 *>(V + at(t0 + i) + 2 * lane);
-            const float w = __shfl(p, i);
-            A->x += w * (float)v[0];
-            A->y += w * (float)v[1];
+        for (int i = 0; i < 8; ++i) {
+            const uint64_t found = __ballot(beyond >> i & 1u);
+#pragma unroll 1
+            for (int r = 0; r < 4; ++r) {
+                if ((found >> (16 * r) & 0xffffu) == 0u) continue;
+                const int j = t0 + 4 * i + r;
+                const T *row = V + at(min(j, last)) + 4 * hi;
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const vec4 x = *reinterpret_cast<const vec4 *>(row + d * 32 + e * 8);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y)
+                            if (j <= my_last && !(fabsf((float)x[y]) < __builtin_inff())) O[d][4 * e + y] += (float)x[y];
+                    }
+            }
         }
     }
 }
@@ -423,16 +483,18 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         __syncthreads();
         bad = *flag != 0u;
     }
-    if (on) {
+    // The lane's half of its row, from weights that carry 2^room: the result, or a part of it.
+    auto write = [&](const auto &g, const Quotient &by_G, float room) {
         l = halves_sum(l);
-        const int own = a.by_G.of(my_row), head = kvh * a.G + my_row - own * a.G;
+        const int own = by_G.of(my_row), head = kvh * g.G + my_row - own * g.G;
         const int64_t token = qs + own;
-        if (a.n_split > 1) {
-            const int64_t row = ((int64_t)blockIdx.y * a.total_q + token) * a.Hq + head;
+        if (g.n_split > 1) {
+            const int64_t row = ((int64_t)blockIdx.y * g.total_q + token) * g.Hq + head;
             if (my_last < 0) m = kNegInf;                // (a part without a key that the row sees)
-            if (hi == 0) a.part_ml[row] = bad ? make_float2(0.0f, __builtin_nanf("")) : make_float2(m, l);
+            // (2^(s - m + room) is 2^(s - (m + kRoom - room) + kRoom))
+            if (hi == 0) g.part_ml[row] = bad ? make_float2(0.0f, __builtin_nanf("")) : make_float2(m + (kRoom - room), l);
             if (l != 0.0f) {
-                float *acc = a.part_acc + row * kD + 4 * hi;
+                float *acc = g.part_acc + row * kD + 4 * hi;
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -442,7 +504,7 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
         } else {
             // (a row whose pages or places are not there is NaN, one that sees no key is zero)
             const float inv = bad ? __builtin_nanf("") : my_last < 0 ? 0.0f : 1.0f / l;
-            T *dst = static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 8 * hi;
+            T *dst = static_cast<T *>(g.out) + token * g.out_stride + (int64_t)head * kD + 8 * hi;
             // (four channels of a lane and the next four of the lane 32 away, exchanged for whole pieces of 16 bytes: 97 tokens of 32
             // heads 8.0 -> 7.4 us, 12 of 300 in groups of 4 32.4 -> 28.4, 8 of 2407 in pairs 443 -> 431.  Whole rows by way of LDS: no better.)
             typedef T vec4 __attribute__((ext_vector_type(4)));
@@ -461,42 +523,36 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
                     *reinterpret_cast<u32x4 *>(dst + d * 32 + i * 8) = (u32x4){u.x, v.x, u.y, v.y};
                 }
         }
-    }
-    // A value that is not finite comes into rows that do not see its key as well, 0 times it being NaN.  So rows whose
-    // numerator is not finite are formed anew without the matrix units, from the keys that they see.  (Nor does it
-    // matter then that the numerator of a row of huge values had overflowed.)  Looked at while the rows above are being written.
+    };
+    if (on) write(a, a.by_G, kRoom);
+    // Rows whose numerator is not finite are formed once more (looked for while they are being written).
     f32x16 all = (O[0] + O[1]) + (O[2] + O[3]);
 #pragma unroll
     for (int n = 8; n > 0; n /= 2)
 #pragma unroll
         for (int i = 0; i < n; ++i) all[i] += all[i + n];
     const uint64_t beyond = __ballot(on && !bad && !(fabsf(all[0]) < __builtin_inff()));
-    const uint32_t anew = (uint32_t)beyond | (uint32_t)(beyond >> 32);
-    if (anew) __threadfence();   // (they are written once more)
-    for (uint32_t left = anew; left; left &= left - 1u) {
-        const int row = r0 + wave * 32 + __builtin_ctz(left), own = a.by_G.of(row), head = kvh * a.G + row - own * a.G;
-        const int64_t token = qs + own;
+    if (const uint32_t anew = (uint32_t)beyond | (uint32_t)(beyond >> 32)) {
+        // (The arguments are read again: those that only this part needs would be kept over the loop, which has no scalar registers
+        //  left for them.)
+        auto *end = (const __attribute__((address_space(4))) PromptArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(end));
+        const Quotient by_G = {end->by_G.m, end->by_G.shift};
+        const int own = by_G.of(min(my_row, n_rows - 1)), head = kvh * end->G + min(my_row, n_rows - 1) - own * end->G;
+        const int last = min(by_G.of(min(r0 + wave * 32 + 31, n_rows - 1)) + before, nk - 1);   // (the rows' last keys ascend)
         auto at = [&](int j) -> int64_t {
             if constexpr (PAGED) {
                 const int t = first_key + j;
-                return ((((int64_t)pages[t >> a.page_log2] * a.Hkv + kvh) << a.page_log2) + (t & ((1 << a.page_log2) - 1))) * kD;
+                return ((((int64_t)pages[t >> end->page_log2] * end->Hkv + kvh) << end->page_log2) + (t & ((1 << end->page_log2) - 1))) * kD;
             } else {
-                return kv0 + j * a.kv_stride;
+                return kv0 + j * end->kv_stride;
             }
         };
-        const int last = min(own + before, nk - 1);
-        float m1, l1;
-        float2 A;
-        row_alone(static_cast<const T *>(a.q) + token * a.q_stride + (int64_t)head * kD, static_cast<const T *>(a.K),
-                  static_cast<const T *>(a.V), last, at, &m1, &l1, &A);
-        if (a.n_split > 1) {
-            const int64_t to = ((int64_t)blockIdx.y * a.total_q + token) * a.Hq + head;
-            if (lane == 0) a.part_ml[to] = make_float2(m1 + kRoom, l1);    // (2^(s - m) is 2^(s - (m + kRoom) + kRoom))
-            *reinterpret_cast<float2 *>(a.part_acc + to * kD + 2 * lane) = A;
-        } else {
-            typedef T vec2 __attribute__((ext_vector_type(2)));
-            *reinterpret_cast<vec2 *>(static_cast<T *>(a.out) + token * a.out_stride + (int64_t)head * kD + 2 * lane) = last < 0 ? (vec2)(T)0.0f : (vec2){(T)(A.x / l1), (T)(A.y / l1)};
-        }
+        float room;
+        // (the tiles are done with; the upper half of a wavefront's quarter of them does not hold the flag above)
+        rows_again<T>(static_cast<const T *>(end->q) + (int64_t)(qs + own) * end->q_stride + (int64_t)head * kD, static_cast<const T *>(end->K),
+                      static_cast<const T *>(end->V), last, my_last, n_clear * kKeys, at, tiles + wave * kPieces + kPieces / 2, &room, &m, &l, O);
+        if (anew >> lo & 1u) write(*end, by_G, room);
     }
 }
 

@@ -484,3 +484,81 @@ def test_few_tiles_of_many_heads(dtype, form, guide):
                 o = slice(int(qs[i]), int(qs[i + 1]))
                 near(out[o], q[o], kv[i][0], kv[i][1], b, t)
         assert torch.equal(out, first)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["packed", "paged"])
+@pytest.mark.parametrize("size", [1e34, 1e35, 3.3895e38])
+def test_over_the_range_of_bf16(size, form):
+    """Values as large as bf16 has, equal ones that add up among them: the result is a number, theirs."""
+    t, code, P, Hq, Hkv, new, before = torch.bfloat16, ds.DS_BF16, 32, 6, 2, [1, 70, 300, 40], [0, 0, 63, 1000]
+    keys = [a + b for a, b in zip(new, before)]
+    T, qs, ks = sum(new), starts(new), starts(keys)
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 51)
+    for i, x in enumerate(kv):
+        v = x[1].float()
+        x[1] = torch.where(torch.arange(D) % 3 == 0, torch.full_like(v, size), v / v.abs().max() * size).to(t)
+        assert torch.isfinite(x[1]).all()
+        for j in range((keys[i] + P - 1) // P):
+            part = x[1, j * P:(j + 1) * P].transpose(0, 1)
+            Vp[table[i + 1, j], :, :part.shape[1]] = part.cuda()
+    q = values((T, Hq, D), t, 1)
+    q[:, 0] = 0.0                                  # (equal weights)
+    K, V = (torch.cat([x[i] for x in kv]).cuda() for i in (0, 1))
+    out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+    prm = ds.prompt(len(new), Hq, Hkv, D, T, 0, code, kv_elems=K.numel())
+    if form == "packed":
+        ds.ds_prompt_attention(q.cuda(), K, V, out, qs.cuda(), ks[:-1].contiguous().cuda(), torch.tensor(keys, dtype=torch.int32).cuda(),
+                               ds.ds_prompt_workspace_alloc(prm), prm)
+    else:
+        pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+        ds.ds_prompt_attention_paged(q.cuda(), Kp, Vp, out, qs.cuda(), torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda(),
+                                     torch.tensor([9] + keys + [9], dtype=torch.int32).cuda(), table, ds.ds_prompt_workspace_alloc(prm), prm, pg)
+    torch.cuda.synchronize()
+    for i, (m, b) in enumerate(zip(new, before)):
+        o = slice(int(qs[i]), int(qs[i + 1]))
+        near(out[o].double().cpu() / size, q[o], kv[i][0], kv[i][1].double() / size, b, t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["packed", "paged"])
+@pytest.mark.parametrize("what", ["first_value", "all_values", "first_key", "queries"])
+def test_cost_of_what_is_not_finite(what, form):
+    """A NaN that all rows of a prompt see, values of which none is finite (each row has hidden ones in its tiles), rows of q that are NaN: all
+    rows are formed twice, which costs a small factor and does not grow with the length as the rows themselves do."""
+    t, code, P, Hq, Hkv, n = torch.float16, ds.DS_F16, 64, 16, 8, 4096
+    q, K, V = values((n, Hq, D), t, 1).cuda(), values((n, Hkv, D), t, 2).cuda(), values((n, Hkv, D), t, 3).cuda()
+    {"first_value": V[0], "all_values": V, "first_key": K[0], "queries": q}[what][..., 5] = math.nan
+    good = values((n, Hkv, D), t, 3).cuda(), values((n, Hkv, D), t, 2).cuda(), values((n, Hq, D), t, 1).cuda()
+    out = torch.empty_like(q)
+    prm = ds.prompt(1, Hq, Hkv, D, n, n, code, kv_elems=K.numel())
+    ws, zero, ends, length = ds.ds_prompt_workspace_alloc(prm), ints_([0]), ints_([0, n]), ints_([n])
+    table = torch.arange(n // P, dtype=torch.int32, device="cuda")[None]
+    pg = ds.pages(n // P, P, Hkv, D, 1, n // P, code)
+    pools = lambda x: x.reshape(n // P, P, Hkv, D).transpose(1, 2).contiguous()  # noqa: E731
+
+    def passes(q, K, V):
+        if form == "paged":
+            K, V = pools(K), pools(V)
+            run = lambda: ds.ds_prompt_attention_paged(q, K, V, out, ends, None, length, table, ws, prm, pg)  # noqa: E731
+        else:
+            run = lambda: ds.ds_prompt_attention(q, K, V, out, ends, zero, length, ws, prm)  # noqa: E731
+        run()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.synchronize()
+        a.record()
+        for _ in range(5):
+            run()
+        b.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(b) / 5
+
+    plain, strange = passes(good[2], good[1], good[0]), passes(q, K, V)
+    print(f"{what} {form}: {1000 * plain:.0f} -> {1000 * strange:.0f} us")
+    touched = torch.isnan(out).any(dim=1)
+    assert touched[:, 5].all() and (what not in ("first_value", "all_values") or not torch.isnan(out[..., :5]).any())
+    assert strange < 20 * plain
+
+
+def ints_(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
