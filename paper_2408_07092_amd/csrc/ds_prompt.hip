@@ -557,7 +557,8 @@ __global__ __launch_bounds__(kWG, 2) void k_prompt(PromptArgs a)
 }
 
 // Joins the parts of split keys, a wavefront for a row of a head:
-//   y = sum_z acc_z 2^(m_z - M) / sum_z l_z 2^(m_z - M),  M = max_z m_z,  z ascending.
+//   y = sum_z acc_z 2^(m_z - M) / sum_z l_z 2^(m_z - M),  M = max_z m_z + 6,  z ascending
+// (parts of large bf16 values add up to more than binary32 holds: 64 of them at most, each with a weight of 1/64 at most, do not).
 template <class T>
 __global__ __launch_bounds__(kWG) void k_prompt_join(PromptArgs a)
 {
@@ -574,7 +575,8 @@ __global__ __launch_bounds__(kWG) void k_prompt_join(PromptArgs a)
     float M = ml.x;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    const float f = ml.x == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(ml.x - M);
+    static_assert(kPromptParts == 1 << 6);
+    const float f = ml.x == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(ml.x - M - 6.0f);
     float L = f * ml.y;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o);

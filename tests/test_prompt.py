@@ -487,11 +487,14 @@ def test_few_tiles_of_many_heads(dtype, form, guide):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("form", ["packed", "paged"])
-@pytest.mark.parametrize("size", [1e34, 1e35, 3.3895e38])
+@pytest.mark.parametrize("form", ["packed", "paged", "split"])
+@pytest.mark.parametrize("size", [3e33, 1e34, 1e35, 3.3895e38])
 def test_over_the_range_of_bf16(size, form):
-    """Values as large as bf16 has, equal ones that add up among them: the result is a number, theirs."""
+    """Values as large as bf16 has, equal ones that add up among them, within a part of split keys and over the parts: the result is a
+    number, theirs."""
     t, code, P, Hq, Hkv, new, before = torch.bfloat16, ds.DS_BF16, 32, 6, 2, [1, 70, 300, 40], [0, 0, 63, 1000]
+    if form == "split":
+        new, before = [3, 20, 1], [1000, 4000, 64]
     keys = [a + b for a, b in zip(new, before)]
     T, qs, ks = sum(new), starts(new), starts(keys)
     Kp, Vp, table, kv = paged(keys, Hkv, P, t, 51)
@@ -506,8 +509,9 @@ def test_over_the_range_of_bf16(size, form):
     q[:, 0] = 0.0                                  # (equal weights)
     K, V = (torch.cat([x[i] for x in kv]).cuda() for i in (0, 1))
     out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
-    prm = ds.prompt(len(new), Hq, Hkv, D, T, 0, code, kv_elems=K.numel())
-    if form == "packed":
+    prm = ds.prompt(len(new), Hq, Hkv, D, T, 60000 if form == "split" else 0, code, kv_elems=K.numel())
+    assert (ds.ds_prompt_workspace_bytes(prm) > 256) == (form == "split")
+    if form != "paged":
         ds.ds_prompt_attention(q.cuda(), K, V, out, qs.cuda(), ks[:-1].contiguous().cuda(), torch.tensor(keys, dtype=torch.int32).cuda(),
                                ds.ds_prompt_workspace_alloc(prm), prm)
     else:
