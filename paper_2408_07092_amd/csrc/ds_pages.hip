@@ -256,14 +256,17 @@ __global__ __launch_bounds__(kWG) void k_pages_free(PagesArgs a)
     for (int i = tid; i < (a.n_rows + 31) / 32; i += kWG) seen[i] = 0u;
     if (tid == 0) s_bad = 0u;
     __syncthreads();
-    for (int i = tid; i < a.n; i += kWG)
-        if (mark(a, seen, a.rows[i])) s_bad = 1u;
+    for (int i = tid; i < a.n; i += kWG) {   // (a length that another workgroup has set to 0 by now was right before)
+        const int r = a.rows[i];
+        const uint32_t code = mark(a, seen, r) ? DS_PAGES_ROWS : length_ok(a, a.lens[r]) ? DS_PAGES_DONE : DS_PAGES_LENGTH;
+        if (code) atomicMax(&s_bad, code);
+    }
     __syncthreads();
-    const bool bad = s_bad != 0u;
-    if (blockIdx.x == 0 && tid == 0) *a.status = bad ? DS_PAGES_ROWS : DS_PAGES_DONE;
+    const uint32_t bad = s_bad;
+    if (blockIdx.x == 0 && tid == 0) *a.status = (int32_t)bad;
     if (bad) return;
     const int row = a.rows[blockIdx.x];
-    const int held = min(pages_in(a, a.lens[row]), a.max_pages);
+    const int held = pages_in(a, a.lens[row]);
     int32_t *entry = a.table + (size_t)row * a.max_pages;
     constexpr int kFlight = 8;
     for (int j0 = tid; j0 < held; j0 += kWG * kFlight) {

@@ -237,6 +237,23 @@ def test_books_at_their_limits():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("length", [-1, -(2**31), 7 * 16 + 1, 2**31 - 1])
+def test_free_reports_a_length_that_cannot_be(length):
+    """... and changes nothing, in whichever place of the list the row is; a row that is none counts for more."""
+    dev, mod = Device(40, 16, 12, 7), Books(40, 16, 12, 7)
+    rows, n = [3, 0, 11, 5], [40, 112, 1, 17]
+    assert dev.extend(rows, n) == mod.extend(rows, n)
+    dev.lens[5] = mod.lens[5] = length
+    for wrong in ([5], [3, 5], [5, 11, 0], [0, 3, 5, 11]):
+        assert dev.free(wrong) == ds.DS_PAGES_LENGTH
+        dev.same(mod)
+    assert dev.free([5, 12]) == ds.DS_PAGES_ROWS and dev.free([5, 3, 5]) == ds.DS_PAGES_ROWS
+    dev.same(mod)
+    assert dev.free([11, 3]) == mod.free([11, 3]) == ds.DS_PAGES_DONE
+    dev.same(mod)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("Hkv", [1, 3, 8])
 @pytest.mark.parametrize("P", [16, 64, 256])
 def test_copy(P, Hkv):
