@@ -288,11 +288,24 @@ __global__ __launch_bounds__(kWG) void k_pages_free(PagesArgs a)
 // those pages went in the workspace: ws[0], and ws[4 + page]; ws[4 + n_pages ..] lists the free ones.
 __global__ __launch_bounds__(kBooks) void k_pages_compact(PagesArgs a, int32_t *ws)
 {
-    __shared__ uint32_t s_w[kBookWaves];
+    __shared__ uint32_t s_w[kBookWaves], s_bad;
     const int tid = threadIdx.x;
     int32_t *map = ws + 4, *holes = map + a.n_pages;
     const Counts counts0(a.refs, a.n_pages, tid * 16);
+    bool bad = !length_ok(a, a.lens[min(tid, a.n_rows - 1)]);
+    if (tid == 0) s_bad = 0u;
+    __syncthreads();
+    for (int r = tid + kBooks; r < a.n_rows; r += kBooks) bad |= !length_ok(a, a.lens[r]);
+    if (bad) s_bad = 1u;   // (seen by all behind the barriers of each_free)
     const int n_live = a.n_pages - (int)each_free(a.refs, a.n_pages, (uint32_t)a.n_pages, s_w, counts0, [](uint32_t, int) {});
+    if (s_bad) {
+        if (tid == 0) {
+            ws[0] = a.n_pages;   // (k_pages_remap finds nothing to do)
+            *a.n_copies = 0;
+            *a.status = DS_PAGES_LENGTH;
+        }
+        return;
+    }
     // holes (free, before n_live) and movers (held, from n_live on), ascending: as many of one as of the other
     uint32_t n_holes = 0, n_movers = 0;
     for (int p0 = 0; p0 < a.n_pages; p0 += kBooks * 16) {

@@ -254,6 +254,24 @@ def test_free_reports_a_length_that_cannot_be(length):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("length", [-1, 7 * 16 + 1, 2**31 - 1])
+@pytest.mark.parametrize("row", [0, 1999])
+def test_compact_reports_a_length_that_cannot_be(row, length):
+    dev, mod = Device(2000, 16, 2000, 7), Books(2000, 16, 2000, 7)
+    rows = [row, 5, 700]
+    assert dev.extend(rows, [40, 112, 17]) == mod.extend(rows, [40, 112, 17])
+    assert dev.free([5]) == mod.free([5]) and dev.extend([3], [20]) == mod.extend([3], [20])
+    dev.lens[row] = mod.lens[row] = length
+    copies, count, status = ints([[77] * 4] * 1001), ints([77]), ints([77])
+    ds.ds_pages_compact(dev.refs, dev.table, dev.lens, copies, count, status, dev.ws, dev.pg)
+    assert status.item() == ds.DS_PAGES_LENGTH and count.item() == 0 and (copies == 77).all()
+    dev.same(mod)
+    dev.lens[row] = mod.lens[row] = 40
+    assert dev.compact() == mod.compact()
+    dev.same(mod)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("Hkv", [1, 3, 8])
 @pytest.mark.parametrize("P", [16, 64, 256])
 def test_copy(P, Hkv):
