@@ -285,7 +285,8 @@ __global__ __launch_bounds__(kWG) void k_pages_free(PagesArgs a)
 }
 
 // The live pages behind the first n_live go to the free ones among them: see ds_pages_compact.  Leaves n_live and where
-// those pages went in the workspace: ws[0], and ws[4 + page]; ws[4 + n_pages ..] lists the free ones.
+// those pages went in the workspace: ws[0], and ws[4 + page], where a page behind the front that nobody holds stays (an entry of the
+// table may name one if the books were not in order); ws[4 + n_pages ..] lists the free ones.
 __global__ __launch_bounds__(kBooks) void k_pages_compact(PagesArgs a, int32_t *ws)
 {
     __shared__ uint32_t s_w[kBookWaves], s_bad;
@@ -318,6 +319,13 @@ __global__ __launch_bounds__(kBooks) void k_pages_compact(PagesArgs a, int32_t *
         uint32_t h = n_holes + (rank & 0xffffu), m = n_movers + (rank >> 16);   // (16384 of each in a round at most)
         for (; hole; hole &= hole - 1u) holes[h++] = mine + __builtin_ctz(hole);
         for (; mover; mover &= mover - 1u) a.copies[m++].x = mine + __builtin_ctz(mover);
+        // (all of them for now: the movers' entries are written below)
+        if (mine >= n_live && mine + 16 <= a.n_pages) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<int4 *>(map + mine + i) = make_int4(mine + i, mine + i + 1, mine + i + 2, mine + i + 3);
+        } else {
+            for (int i = max(mine, n_live); i < min(mine + 16, a.n_pages); ++i) map[i] = i;
+        }
         n_holes += total & 0xffffu;
         n_movers += total >> 16;
     }

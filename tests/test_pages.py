@@ -272,6 +272,24 @@ def test_compact_reports_a_length_that_cannot_be(row, length):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n_pages", [50, 16384 + 50])
+def test_compact_leaves_entries_of_pages_that_nobody_holds(n_pages):
+    """... which books in order do not have: what the workspace held before does not get into the table."""
+    dev, mod = Device(n_pages, 16, 4, 30), Books(n_pages, 16, 4, 30)
+    for r, p in ((0, n_pages - 1), (0, n_pages - 2), (1, 7), (1, n_pages - 5), (2, 1)):
+        at = mod.lens[r] // 16
+        mod.table[r][at] = dev.table[r, at] = p
+        mod.lens[r] += 16
+        if p != n_pages - 2:
+            mod.refs[p] = 1
+    dev.refs, dev.lens = ints(mod.refs), ints(mod.lens)
+    dev.ws.fill_(0x11)
+    assert dev.compact() == mod.compact()
+    dev.same(mod)
+    assert dev.table[0, 1].item() == n_pages - 2
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("Hkv", [1, 3, 8])
 @pytest.mark.parametrize("P", [16, 64, 256])
 def test_copy(P, Hkv):
