@@ -165,18 +165,19 @@ def _dp(t):
 
 # (The calls of the paged cache are small, and a step makes many: they pass addresses as plain integers, which costs
 #  a third of a ctypes object.)
-def _at(t):
-    """Address of a contiguous tensor, or NULL."""
-    if t is None:
-        return None
-    if not t.is_contiguous():
-        raise ValueError("tensor must be contiguous")
-    return t.data_ptr()
-
-
-def _vp(t):
-    """Address of a tensor whose strides the call is told of, or NULL."""
-    return None if t is None else t.data_ptr()
+def _at(where: str, device: int, *tensors, dense=True):
+    """Addresses of tensors (None: NULL), each on `device`, and contiguous unless the call is told its strides."""
+    found = []
+    for t in tensors:
+        if t is None:
+            found.append(None)
+        elif t.get_device() != device or device < 0:   # (-1: memory of the host)
+            raise ValueError(f"{where}: a tensor is on {t.device}, which is not the current device")
+        elif dense and not t.is_contiguous():
+            raise ValueError("tensor must be contiguous")
+        else:
+            found.append(t.data_ptr())
+    return found
 
 
 def _bytes(t) -> int:
@@ -187,8 +188,11 @@ def _cleared(n: int, where: str, device):
     if n == 0:
         raise DsError(DS_ERR_SHAPE, where)
     ws = torch.empty(n, dtype=torch.uint8, device=device)
-    ds_workspace_init(ws)
-    torch.cuda.current_stream(ws.device).synchronize()
+    if ws.get_device() < 0:
+        raise ValueError(f"{where}: a workspace is memory of a GPU, not on {ws.device}")
+    with torch.cuda.device(ws.device):
+        ds_workspace_init(ws)
+        torch.cuda.current_stream().synchronize()
     return ws
 
 
@@ -199,11 +203,10 @@ def _stream(stream=None):
     return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
-def _stream_of(t, where: str, stream=None):
-    """The stream of a call whose tensors are where `t` is, which has to be the current device."""
-    device = t.get_device()   # (-1: memory of the host)
-    if device < 0 or device != torch._C._cuda_getDevice():
-        raise ValueError(f"{where}: a tensor is on {t.device}, which is not the current device")
+def _stream_of(device: int, where: str, stream=None):
+    """The stream of a call whose tensors are on `device`, which has to be the current one."""
+    if device != torch._C._cuda_getDevice() or (stream is not None and stream.device_index != device):
+        raise ValueError(f"{where}: its tensors are on GPU {device}, which is not the current device or not the stream's")
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
@@ -415,17 +418,20 @@ def ds_prompt_workspace_alloc(prm: DsPrompt, device="cuda") -> "torch.Tensor":
 
 def ds_prompt_attention(q, K, V, out, q_start, kv_start, kv_len, workspace, prm: DsPrompt, stream=None):
     """q, K, V and out may be views with the strides that `prm` names."""
-    _check(lib().ds_prompt_attention(_vp(q), _vp(K), _vp(V), _vp(out), _at(q_start), _at(kv_start), _at(kv_len),
-                                     _at(workspace), _bytes(workspace), ctypes.byref(prm), _stream_of(q, "ds_prompt_attention", stream)),
-           "ds_prompt_attention")
+    where, dev = "ds_prompt_attention", q.get_device()
+    _check(lib().ds_prompt_attention(*_at(where, dev, q, K, V, out, dense=False),
+                                     *_at(where, dev, q_start, kv_start, kv_len, workspace), _bytes(workspace),
+                                     ctypes.byref(prm), _stream_of(dev, where, stream)), where)
 
 
 def ds_prompt_attention_paged(q, K_pages, V_pages, out, q_start, rows, lens, table, workspace, prm: DsPrompt,
                               pages: DsPages, stream=None):
-    _check(lib().ds_prompt_attention_paged(_vp(q), _at(K_pages), _at(V_pages), _vp(out), _at(q_start), _at(rows),
-                                           _at(lens), _at(table), _at(workspace), _bytes(workspace),
-                                           ctypes.byref(prm), ctypes.byref(pages), _stream_of(q, "ds_prompt_attention_paged", stream)),
-           "ds_prompt_attention_paged")
+    where, dev = "ds_prompt_attention_paged", q.get_device()
+    _check(lib().ds_prompt_attention_paged(*_at(where, dev, q, dense=False), *_at(where, dev, K_pages, V_pages),
+                                           *_at(where, dev, out, dense=False),
+                                           *_at(where, dev, q_start, rows, lens, table, workspace),
+                                           _bytes(workspace), ctypes.byref(prm), ctypes.byref(pages),
+                                           _stream_of(dev, where, stream)), where)
 
 
 def ds_paged_workspace_bytes(pages: DsPages, n_seqs: int, Hq: int, max_len: int) -> int:
@@ -439,33 +445,39 @@ def ds_paged_workspace_alloc(pages: DsPages, n_seqs: int, Hq: int, max_len: int,
 
 def ds_paged_decode(q, K_pages, V_pages, out, rows, lens, table, workspace, pages: DsPages, n_seqs: int, Hq: int,
                     max_len: int, stream=None):
-    _check(lib().ds_paged_decode(_at(q), _at(K_pages), _at(V_pages), _at(out), _at(rows), _at(lens), _at(table),
-                                 _at(workspace), _bytes(workspace), ctypes.byref(pages), n_seqs, Hq, max_len,
-                                 _stream_of(q, "ds_paged_decode", stream)), "ds_paged_decode")
+    where, dev = "ds_paged_decode", q.get_device()
+    _check(lib().ds_paged_decode(*_at(where, dev, q, K_pages, V_pages, out, rows, lens, table, workspace),
+                                 _bytes(workspace), ctypes.byref(pages), n_seqs, Hq, max_len,
+                                 _stream_of(dev, where, stream)), where)
 
 
 def ds_append_paged(k_new, v_new, K_pages, V_pages, new_start, rows, start, table, pages: DsPages, n_seqs: int,
                     stream=None):
     """k_new, v_new [total_new, Hkv, d], dense or views that step the same from token to token."""
     assert k_new.shape[0] == v_new.shape[0] and k_new.stride() == v_new.stride() and k_new.stride()[1:] == (pages.d, 1)
-    _check(lib().ds_append_paged(_vp(k_new), _vp(v_new), _at(K_pages), _at(V_pages), _at(new_start), _at(rows),
-                                 _at(start), _at(table), ctypes.byref(pages), n_seqs, k_new.shape[0], k_new.stride(0),
-                                 _stream_of(k_new, "ds_append_paged", stream)), "ds_append_paged")
+    where, dev = "ds_append_paged", k_new.get_device()
+    _check(lib().ds_append_paged(*_at(where, dev, k_new, v_new, dense=False),
+                                 *_at(where, dev, K_pages, V_pages, new_start, rows, start, table),
+                                 ctypes.byref(pages), n_seqs, k_new.shape[0], k_new.stride(0),
+                                 _stream_of(dev, where, stream)), where)
 
 
 def ds_pages_extend(refs, table, lens, rows, n_new, start, status, pages: DsPages, n: int, stream=None):
-    _check(lib().ds_pages_extend(_at(refs), _at(table), _at(lens), _at(rows), _at(n_new), _at(start), _at(status),
-                                 ctypes.byref(pages), n, _stream_of(refs, "ds_pages_extend", stream)), "ds_pages_extend")
+    where, dev = "ds_pages_extend", refs.get_device()
+    _check(lib().ds_pages_extend(*_at(where, dev, refs, table, lens, rows, n_new, start, status),
+                                 ctypes.byref(pages), n, _stream_of(dev, where, stream)), where)
 
 
 def ds_pages_fork(refs, table, lens, src, dst, copies, n_copies, status, pages: DsPages, n: int, stream=None):
-    _check(lib().ds_pages_fork(_at(refs), _at(table), _at(lens), _at(src), _at(dst), _at(copies), _at(n_copies),
-                               _at(status), ctypes.byref(pages), n, _stream_of(refs, "ds_pages_fork", stream)), "ds_pages_fork")
+    where, dev = "ds_pages_fork", refs.get_device()
+    _check(lib().ds_pages_fork(*_at(where, dev, refs, table, lens, src, dst, copies, n_copies, status),
+                               ctypes.byref(pages), n, _stream_of(dev, where, stream)), where)
 
 
 def ds_pages_free(refs, table, lens, rows, status, pages: DsPages, n: int, stream=None):
-    _check(lib().ds_pages_free(_at(refs), _at(table), _at(lens), _at(rows), _at(status), ctypes.byref(pages), n,
-                               _stream_of(refs, "ds_pages_free", stream)), "ds_pages_free")
+    where, dev = "ds_pages_free", refs.get_device()
+    _check(lib().ds_pages_free(*_at(where, dev, refs, table, lens, rows, status), ctypes.byref(pages), n,
+                               _stream_of(dev, where, stream)), where)
 
 
 def ds_pages_workspace_bytes(pages: DsPages) -> int:
@@ -478,11 +490,12 @@ def ds_pages_workspace_alloc(pages: DsPages, device="cuda") -> "torch.Tensor":
 
 
 def ds_pages_compact(refs, table, lens, copies, n_copies, status, workspace, pages: DsPages, stream=None):
-    _check(lib().ds_pages_compact(_at(refs), _at(table), _at(lens), _at(copies), _at(n_copies), _at(status),
-                                  _at(workspace), _bytes(workspace), ctypes.byref(pages), _stream_of(refs, "ds_pages_compact", stream)),
-           "ds_pages_compact")
+    where, dev = "ds_pages_compact", refs.get_device()
+    _check(lib().ds_pages_compact(*_at(where, dev, refs, table, lens, copies, n_copies, status, workspace),
+                                  _bytes(workspace), ctypes.byref(pages), _stream_of(dev, where, stream)), where)
 
 
 def ds_pages_copy(K_pages, V_pages, copies, n_copies, pages: DsPages, max_copies: int, stream=None):
-    _check(lib().ds_pages_copy(_at(K_pages), _at(V_pages), _at(copies), _at(n_copies), ctypes.byref(pages), max_copies,
-                               _stream_of(K_pages, "ds_pages_copy", stream)), "ds_pages_copy")
+    where, dev = "ds_pages_copy", K_pages.get_device()
+    _check(lib().ds_pages_copy(*_at(where, dev, K_pages, V_pages, copies, n_copies), ctypes.byref(pages),
+                               max_copies, _stream_of(dev, where, stream)), where)

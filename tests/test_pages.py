@@ -180,6 +180,64 @@ def test_tensors_off_the_device_are_refused():
             call()
 
 
+class Placed:
+    """What a call asks of a tensor before a launch: where it is and what shape it has."""
+    def __init__(self, device, shape=(4, 1, D), dtype=2):
+        self.at, self.shape, self.dtype, self.device = device, shape, dtype, f"place {device}"
+
+    def get_device(self):
+        return self.at
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x10000
+
+    def stride(self, i=None):
+        return (D, D, 1) if i is None else (D, D, 1)[i]
+
+    def numel(self):
+        return 1 << 20
+
+    def element_size(self):
+        return self.dtype
+
+
+@pytest.mark.parametrize("where", [-1, 1])      # (the host; another device)
+def test_every_tensor_of_a_call_is_looked_at(monkeypatch, where):
+    """One tensor that is not on the current device, in each place of each call: refused ahead of the library, and so is a stream
+    of another device."""
+    reached = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: reached.append(name) or 0
+    monkeypatch.setattr(ds.binding, "lib", lambda: Library())
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    pg, prm = ds.pages(1, 16, 1, D, 1, 1), ds.prompt(1, 1, 1, D, 1, 1)
+    stream = type("Stream", (), {"device_index": 1, "device": "place 1", "cuda_stream": 0})()
+    for f, n, more in ((ds.ds_prompt_attention, 8, (prm,)), (ds.ds_prompt_attention_paged, 9, (prm, pg)), (ds.ds_paged_decode, 8, (pg, 1, 1, 1)),
+                       (ds.ds_append_paged, 8, (pg, 1)), (ds.ds_pages_extend, 7, (pg, 1)), (ds.ds_pages_fork, 8, (pg, 1)),
+                       (ds.ds_pages_free, 5, (pg, 1)), (ds.ds_pages_compact, 7, (pg,)), (ds.ds_pages_copy, 4, (pg, 1))):
+        f(*[Placed(0)] * n, *more)
+        assert reached.pop() == f.__name__
+        for i in range(n):
+            with pytest.raises(ValueError, match="not the current device"):
+                f(*[Placed(where if j == i else 0) for j in range(n)], *more)
+        with pytest.raises(ValueError, match="not the current device"):
+            f(*[Placed(0)] * n, *more, stream=stream)
+        assert not reached, f.__name__
+
+
+def test_workspaces_are_memory_of_a_gpu():
+    for alloc in (lambda: ds.ds_prompt_workspace_alloc(ds.prompt(1, 1, 1, D, 1, 1), "cpu"), lambda: ds.ds_paged_workspace_alloc(ds.pages(1, 16, 1, D, 1, 1), 1, 1, 1, "cpu"),
+                  lambda: ds.ds_pages_workspace_alloc(ds.pages(1, 16, 1, D, 1, 1), "cpu")):
+        with pytest.raises(ValueError, match="memory of a GPU"):
+            alloc()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n_pages,P,n_rows,max_pages", [(1, 16, 3, 2), (40, 16, 12, 7), (900, 32, 30, 60), (17000, 16, 70, 700), (40000, 256, 40, 1500)])
 def test_books_against_the_model(n_pages, P, n_rows, max_pages):
