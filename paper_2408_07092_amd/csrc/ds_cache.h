@@ -59,7 +59,7 @@ struct PromptPlan {
     int G, n_tiles, n_split;
     size_t off_acc, total;
 };
-bool make_prompt_plan(const ds_prompt_t &m, PromptPlan *p);
+void make_prompt_plan(const ds_prompt_t &m, PromptPlan *p);
 hipError_t launch_prompt(PromptArgs a, bool paged, int dtype, hipStream_t st);
 
 // Row tiles of packed sequences, numbered without a prefix sum: sequence s has its tiles from number

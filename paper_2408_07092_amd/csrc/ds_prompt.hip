@@ -602,7 +602,7 @@ __global__ __launch_bounds__(kWG) void k_prompt_join(PromptArgs a)
 }
 
 // ---------------------------------------------------------------- launcher
-bool make_prompt_plan(const ds_prompt_t &m, PromptPlan *p)
+void make_prompt_plan(const ds_prompt_t &m, PromptPlan *p)
 {
     p->G = m.Hq / m.Hkv;
     p->n_tiles = (int)((int64_t)m.total_q * p->G / kPromptRows) + m.n_seqs;
@@ -625,7 +625,6 @@ bool make_prompt_plan(const ds_prompt_t &m, PromptPlan *p)
     const size_t rows = (size_t)m.total_q * m.Hq * p->n_split;
     p->off_acc = p->n_split > 1 ? (rows * 8 + 255) / 256 * 256 : 0;
     p->total = p->off_acc + (p->n_split > 1 ? rows * kD * 4 : 256);
-    return true;
 }
 
 typedef void (*PromptFn)(PromptArgs);
