@@ -375,8 +375,9 @@ typedef struct {
     int32_t dtype, reserved;              /* ds_dtype_t of the pools; 0                                  */
 } ds_pages_t;
 
-/* Bytes of workspace that a prompt call needs (a multiple of 256).  It need not be cleared, and serves every
- * call that it is large enough for.  Pure host function; 0 if the shape is invalid. */
+/* Bytes of workspace of a prompt call's fastest plan (a multiple of 256), more for few rows over many keys than for many rows.  A call
+ * that is given less, 256 bytes at least, splits its keys into fewer parts (the last bits of a sum can then differ), so one workspace serves
+ * all prompts.  It need not be cleared.  Pure host function; 0 if the shape is invalid. */
 size_t ds_prompt_workspace_bytes(const ds_prompt_t *prm);
 ds_status_t ds_prompt_attention(const void *q, const void *K, const void *V, void *out,
                                 const int32_t *q_start, const int32_t *kv_start, const int32_t *kv_len,

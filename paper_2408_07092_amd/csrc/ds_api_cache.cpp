@@ -94,7 +94,7 @@ ds_status_t ds_prompt_attention(const void *q, const void *K, const void *V, voi
     ds_prompt_t m;
     PromptPlan p;
     if (!prompt_ok(prm, &m)) return DS_ERR_SHAPE;
-    make_prompt_plan(m, &p);
+    make_prompt_plan(m, &p, workspace_bytes);
     if (!aligned(q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(workspace, 16) ||
         !aligned(q_start, 4) || !aligned(kv_start, 4) || !aligned(kv_len, 4))
         return DS_ERR_ALIGN;
@@ -117,7 +117,7 @@ ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const 
     PromptPlan p;
     if (!prompt_ok(prm, &m) || !pages_ok(pages)) return DS_ERR_SHAPE;
     if (pages->Hkv != m.Hkv || pages->dtype != m.dtype || (!rows && m.n_seqs > pages->n_rows)) return DS_ERR_SHAPE;
-    make_prompt_plan(m, &p);
+    make_prompt_plan(m, &p, workspace_bytes);
     if (!aligned(q, 16) || !aligned(K_pages, 256) || !aligned(V_pages, 256) || !aligned(out, 16) ||
         !aligned(workspace, 16) || !aligned(q_start, 4) || !aligned(rows, 4) || !aligned(lens, 4) || !aligned(table, 4))
         return DS_ERR_ALIGN;

@@ -59,7 +59,7 @@ struct PromptPlan {
     int G, n_tiles, n_split;
     size_t off_acc, total;
 };
-void make_prompt_plan(const ds_prompt_t &m, PromptPlan *p);
+void make_prompt_plan(const ds_prompt_t &m, PromptPlan *p, size_t workspace_bytes = SIZE_MAX);   // total: 256 at least
 hipError_t launch_prompt(PromptArgs a, bool paged, int dtype, hipStream_t st);
 
 // Row tiles of packed sequences, numbered without a prefix sum: sequence s has its tiles from number

@@ -602,7 +602,7 @@ __global__ __launch_bounds__(kWG) void k_prompt_join(PromptArgs a)
 }
 
 // ---------------------------------------------------------------- launcher
-void make_prompt_plan(const ds_prompt_t &m, PromptPlan *p)
+void make_prompt_plan(const ds_prompt_t &m, PromptPlan *p, size_t workspace_bytes)
 {
     p->G = m.Hq / m.Hkv;
     p->n_tiles = (int)((int64_t)m.total_q * p->G / kPromptRows) + m.n_seqs;
@@ -615,16 +615,18 @@ void make_prompt_plan(const ds_prompt_t &m, PromptPlan *p)
     const int64_t wgs = (int64_t)p->n_tiles * m.Hkv, most = std::min<int64_t>(2 * device_caps().cus / wgs, kPromptParts);
     const double steps = 1.2 * m.max_kv / kKeys, row_part = (double)m.total_q * m.Hq * (2 * kD * 4) / 3e6;
     double best = steps;
+    p->off_acc = 0;
+    p->total = 256;
     for (int n = 2; n <= most; ++n) {
         const double us = steps / n + 4.0 + n * row_part;
-        if (us < best) {
+        const size_t rows = (size_t)m.total_q * m.Hq * n, off_acc = (rows * 8 + 255) / 256 * 256, total = off_acc + rows * kD * 4;
+        if (us < best && total <= workspace_bytes) {    // (what the parts do not fit in, fewer do, and none always)
             best = us;
             p->n_split = n;
+            p->off_acc = off_acc;
+            p->total = total;
         }
     }
-    const size_t rows = (size_t)m.total_q * m.Hq * p->n_split;
-    p->off_acc = p->n_split > 1 ? (rows * 8 + 255) / 256 * 256 : 0;
-    p->total = p->off_acc + (p->n_split > 1 ? rows * kD * 4 : 256);
 }
 
 typedef void (*PromptFn)(PromptArgs);

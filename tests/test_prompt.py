@@ -564,5 +564,34 @@ def test_cost_of_what_is_not_finite(what, form):
     assert strange < 20 * plain
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["packed", "paged"])
+def test_a_workspace_of_another_prompt(form):
+    """That of a long prompt, which is the least that there is, serves a short part over many keys, and so does any size between that and
+    the part's own: with fewer parts, within its bytes."""
+    t, code, P, Hq, Hkv, new, before = torch.float16, ds.DS_F16, 16, 8, 2, [3, 16], [2000, 5000]
+    keys = [a + b for a, b in zip(new, before)]
+    T, qs, ks = sum(new), starts(new), starts(keys)
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 52)
+    q, K, V = values((T, Hq, D), t, 1).cuda(), torch.cat([x[0] for x in kv]).cuda(), torch.cat([x[1] for x in kv]).cuda()
+    prm = ds.prompt(2, Hq, Hkv, D, T, max(keys), code, kv_elems=K.numel())
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    long = ds.ds_prompt_workspace_bytes(ds.prompt(1, Hq, Hkv, D, 8192, 8192, code, kv_elems=K.numel()))
+    need = ds.ds_prompt_workspace_bytes(prm)
+    assert long == 256 and need > 8 * T * Hq * 520
+    for size in (long, 2 * T * Hq * 520, 3 * T * Hq * 520 + 255, need - 1, need, need + 999):
+        ws = torch.full((size + 64,), 0x5a, dtype=torch.uint8, device="cuda")
+        out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+        if form == "packed":
+            ds.ds_prompt_attention(q, K, V, out, qs.cuda(), ks[:-1].contiguous().cuda(), ints_(keys), ws[:size], prm)
+        else:
+            ds.ds_prompt_attention_paged(q, Kp, Vp, out, qs.cuda(), ints_([1, 2]), ints_([9] + keys + [9]), table, ws[:size], prm, pg)
+        torch.cuda.synchronize()
+        assert (ws[size:] == 0x5a).all()
+        for i, (m, b) in enumerate(zip(new, before)):
+            o = slice(int(qs[i]), int(qs[i + 1]))
+            near(out[o], q[o], kv[i][0], kv[i][1], b, t)
+
+
 def ints_(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
