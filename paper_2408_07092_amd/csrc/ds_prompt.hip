@@ -77,10 +77,11 @@ __device__ __forceinline__ float halves_sum(float v)
 
 // Sixteen bytes of every lane, at base + off bytes, from memory into LDS past the registers: to `at` (bytes, the wavefront's)
 // + 16 lane.  Written out because the compiler, not knowing which buffer a transposing read reads, would wait for every
-// load in flight ahead of each of them; the loads are waited for by wait_tiles.  (m0 is the place in LDS.)
+// load in flight ahead of each of them; the loads are waited for by wait_tiles.  (m0, the place in LDS, is used for
+// nothing else in this kernel.)
 __device__ __forceinline__ void load_to_lds(const void *base, uint32_t off, uint32_t at)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(off), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(off), "s"(base) : "memory");
 }
 __device__ __forceinline__ void wait_tiles()
 {
