@@ -340,9 +340,10 @@ ds_status_t ds_attend_rows(const void *q, const void *KV_rows, float *out,
  * n_seqs < 1, total_q < 0, max_kv < 0, bad heads, d != 128, a stride below the row it steps over or
  * beyond 2^30 (kv_stride: 2^24, kv_head_stride: 2^40), an unknown dtype, or (total_q / 128 + n_seqs) * Hq of
  * 2^24 or more -> DS_ERR_SHAPE.  What is on the device is checked there: a sequence whose new tokens do not
- * lie in [0, total_q) is not computed (its rows are left as they are), one whose keys do not lie within kv_elems,
- * within its row of the page table or on pages of the pool, or are more than 2^30, gets NaN, and nothing is
- * read outside.
+ * lie in [0, total_q) is not computed (its rows are left as they are), one whose keys do not lie within kv_elems
+ * or within its row of the page table, or are more than 2^30, gets NaN, and nothing is read outside.  Of a sequence with a
+ * page that is none of the pool's, the rows that see a key on it get NaN; so do rows before them which share a tile with it, of
+ * 128 rows (token * G + head of the group) or 64 keys, and the others are computed.
  * Keys that a row does not see have no part in it, whatever they and their values hold, infinities and NaN
  * too.  Rows that see such a value, or stand beside one in a tile, and rows whose sums overflow (bf16) are formed a second time,
  * after which sums of finite values are finite; a call all of whose rows are takes some five times as long.

@@ -593,5 +593,45 @@ def test_a_workspace_of_another_prompt(form):
             near(out[o], q[o], kv[i][0], kv[i][1], b, t)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("guide", [0, 60000])
+@pytest.mark.parametrize("heads", [(8, 2), (2, 2), (6, 1)], ids=str)
+def test_which_rows_a_missing_page_makes_nan(heads, guide):
+    """Those of the row tiles whose key tiles reach it: every row that sees it, none of the tiles before."""
+    t, code, P, (Hq, Hkv), new, before = torch.float16, ds.DS_F16, 16, heads, [3, 300, 40], [20, 41, 0]
+    G, keys = Hq // Hkv, [a + b for a, b in zip(new, before)]
+    T, qs = sum(new), starts(new)
+    if guide:
+        new, T, qs = [3, 100, 40], 143, starts([3, 100, 40])
+        before = [20, 241, 0]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 53)
+    q, rows, lens = values((T, Hq, D), t, 1).cuda(), ints_([1, 2, 3]), ints_([9] + keys + [9])
+    prm = ds.prompt(3, Hq, Hkv, D, T, guide, code)
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    ws = ds.ds_prompt_workspace_alloc(prm)
+    assert (ws.numel() > 256) == (guide > 0)
+    for page in (0, 2, 5, 12, 17, 21):
+        tb = table.clone()
+        tb[2, page] = (Kp.shape[0], -1)[page % 2]
+        out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+        ds.ds_prompt_attention_paged(q, Kp, Vp, out, qs.cuda(), rows, lens, tb, ws, prm, pg)
+        torch.cuda.synchronize()
+        want = torch.zeros((new[1], Hkv, G), dtype=torch.bool)
+        for i in range(new[1]):
+            for g in range(G):
+                last = (min((i * G + g) // 128 * 128 + 128, new[1] * G) - 1) // G           # the tile's last token
+                reach = min(keys[1], (last + before[1] + 64) // 64 * 64)
+                want[i, :, g] = page * P < reach
+                assert want[i, 0, g] or page * P > i + before[1]
+        mine = out[int(qs[1]):int(qs[2])].cpu()
+        want = want.reshape(new[1], Hq)
+        assert torch.equal(torch.isnan(mine).any(dim=2), want) and torch.equal(torch.isnan(mine).all(dim=2), want)
+        free = int((~want.any(dim=1)).sum())                                                # (rows of the tiles before come first)
+        near(mine[:free], q[int(qs[1]):int(qs[1]) + free], kv[1][0][:free + before[1]], kv[1][1][:free + before[1]], before[1], t)
+        for i in (0, 2):
+            o = slice(int(qs[i]), int(qs[i + 1]))
+            near(out[o], q[o], kv[i][0], kv[i][1], before[i], t)
+
+
 def ints_(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
