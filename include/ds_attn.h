@@ -395,6 +395,8 @@ ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const 
  * Lengths are read on the device, so a captured call follows them; max_len (>= 0) is the length that the launch
  * and the workspace are sized for, a guide that the results do not rest on, but bits of a sum may.  A sequence without a token gives
  * zeros; one whose row, length or pages cannot be gives NaN, and nothing is read outside the table and the pools.
+ * Weights are the sum of two numbers of the pools' type (22 bits in fp16, 16 in bf16), all sums and statistics binary32.  A value of
+ * a sequence that is infinite or NaN makes its channel infinite or NaN in the heads of its KV head, and touches nothing else.
  * Pools 256-byte aligned, q, out and workspace 16-byte.  n_seqs, Hq < 1, bad heads, rows NULL with n_seqs > n_rows,
  * or n_seqs * Hkv * ceil(G / 16) * (ceil(max_pages * page_tokens / 64) + 3) beyond 2^31 -> DS_ERR_SHAPE.
  * The workspace is cleared once (ds_workspace_init); it then serves every call of the same Hq and Hkv, of any n_seqs,

@@ -237,6 +237,31 @@ def test_decode_over_the_range_of_bf16(size, guide):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("guide", [0, 20000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decode_values_that_are_not_finite(dtype, guide):
+    """An infinite or NaN value is in the result of its own channel and KV head, in whichever tile and part it lies, and nowhere else."""
+    t, code = TYPES[dtype]
+    Hq, Hkv, P, keys = 8, 2, 32, [3000, 17, 500, 1, 65, 2000]
+    Kp, Vp, table, kv = paged(keys, Hkv, P, t, 37)
+    q = values((len(keys), Hq, D), t, 1)
+    touched = torch.zeros((len(keys), Hq, D), dtype=torch.bool)
+    for i, token, head, channel, x in ((0, 2999, 0, 5, math.inf), (0, 100, 1, 77, -math.inf), (1, 16, 1, 0, math.nan), (2, 0, 0, 127, -math.inf),
+                                       (4, 64, 0, 9, math.inf), (4, 3, 0, 9, -math.inf), (5, 1024, 1, 64, math.inf)):
+        Vp[table[i + 1, token // P], head, token % P, channel] = x
+        touched[i, head * Hq // Hkv:(head + 1) * Hq // Hkv, channel] = True
+    lens, rows = torch.tensor([7] + keys + [7], dtype=torch.int32).cuda(), torch.arange(1, len(keys) + 1, dtype=torch.int32).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, table.shape[0], table.shape[1], code)
+    out = torch.full((len(keys), Hq, D), CANARY, device="cuda")
+    ds.ds_paged_decode(q.cuda(), Kp, Vp, out, rows, lens, table, ds.ds_paged_workspace_alloc(pg, len(keys), Hq, guide), pg, len(keys), Hq, guide)
+    got = out.cpu()
+    assert torch.equal(~torch.isfinite(got), touched)
+    for i in range(len(keys)):      # (those channels: as if the value were a number, which the others do not depend on)
+        y = defined(q[i][None], kv[i][0], kv[i][1], keys[i] - 1)[0][0].float()
+        near(torch.where(touched[i], y, got[i]), q[i], kv[i][0], kv[i][1], t)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("heads", [(2, 2), (24, 2)], ids=str)
 def test_decode_workspace_serves_other_batches(heads):
     """One workspace, cleared once, for more and fewer sequences in turn: what one call leaves of its parts is not where
