@@ -414,7 +414,7 @@ ds_status_t ds_paged_decode(const void *q, const void *K_pages, const void *V_pa
  * total_new of them) become tokens start[s], start[s] + 1, .. of table row rows[s] (NULL: row s).  new_start
  * [n_seqs + 1], start [n_seqs] int32 on the device; start[s] < 0: nothing is written for s.  The pages have to be in the table
  * (ds_pages_extend); what has no page of the pool is not written.  Rows are distinct.  total_new * ceil(Hkv / 8)
- * is less than 2^26, else DS_ERR_SHAPE.
+ * is at most 2^26 - 4, else DS_ERR_SHAPE.
  */
 ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages, void *V_pages,
                             const int32_t *new_start, const int32_t *rows, const int32_t *start,

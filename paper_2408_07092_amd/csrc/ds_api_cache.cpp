@@ -195,7 +195,8 @@ ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages,
     const int64_t row = (int64_t)pages->Hkv * kD;
     if (new_stride == 0) new_stride = row;
     if (new_stride < row || new_stride % 8 != 0 || new_stride > 1ll << 30) return DS_ERR_SHAPE;
-    if ((int64_t)total_new * ((pages->Hkv + 7) / 8) >= 1ll << 26) return DS_ERR_SHAPE;
+    // (four wavefronts to a workgroup, and a launch holds less than 2^32 threads)
+    if ((int64_t)total_new * ((pages->Hkv + 7) / 8) > (1ll << 26) - 4) return DS_ERR_SHAPE;
     if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(K_pages, 256) || !aligned(V_pages, 256) ||
         !aligned(new_start, 4) || !aligned(rows, 4) || !aligned(start, 4) || !aligned(table, 4))
         return DS_ERR_ALIGN;

@@ -67,6 +67,14 @@ def test_append_refusals():
     assert append(ok, total=0) == ds.DS_OK
 
 
+def test_append_refuses_what_no_launch_holds():
+    """Wavefronts in fours: the last three counts below 2^26 would fill a launch of 2^32 threads."""
+    for Hkv, parts in ((2, 1), (8, 1), (9, 2), (128, 16)):
+        pg = ds.pages(**{**PG, "Hkv": Hkv})
+        for total in (((1 << 26) - 4) // parts + 1, ((1 << 26) - 1) // parts):
+            assert total * parts <= (1 << 26) - 4 or append(pg, total=total) == ds.DS_ERR_SHAPE, (Hkv, total)
+
+
 # ------------------------------------------------------------------ decode
 def near(got, q, k, v, dtype):
     n = k.shape[0]
