@@ -451,14 +451,24 @@ def ds_paged_decode(q, K_pages, V_pages, out, rows, lens, table, workspace, page
                                  _stream_of(dev, where, stream)), where)
 
 
+def _rows_of(x, pages: DsPages):
+    """Tokens of new rows, and the elements from one to the next (0 where there is no next: a dimension of one has any stride)."""
+    n, heads, d = x.shape
+    if heads < pages.Hkv or d != pages.d or (d > 1 and x.stride(2) != 1) or (heads > 1 and x.stride(1) != d):
+        raise ValueError("new rows must be [tokens, Hkv, d] with dense heads")
+    return n, x.stride(0) if n > 1 else 0
+
+
 def ds_append_paged(k_new, v_new, K_pages, V_pages, new_start, rows, start, table, pages: DsPages, n_seqs: int,
                     stream=None):
     """k_new, v_new [total_new, Hkv, d], dense or views that step the same from token to token."""
-    assert k_new.shape[0] == v_new.shape[0] and k_new.stride() == v_new.stride() and k_new.stride()[1:] == (pages.d, 1)
+    n, step = _rows_of(k_new, pages)
+    if (n, step) != _rows_of(v_new, pages):
+        raise ValueError("k_new and v_new must have the same tokens and step the same")
     where, dev = "ds_append_paged", k_new.get_device()
     _check(lib().ds_append_paged(*_at(where, dev, k_new, v_new, dense=False),
                                  *_at(where, dev, K_pages, V_pages, new_start, rows, start, table),
-                                 ctypes.byref(pages), n_seqs, k_new.shape[0], k_new.stride(0),
+                                 ctypes.byref(pages), n_seqs, n, step,
                                  _stream_of(dev, where, stream)), where)
 
 

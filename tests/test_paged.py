@@ -346,3 +346,38 @@ def test_append(P, Hkv):
     ds.ds_append_paged(k, v, K, V, new_start.cuda(), rows.cuda(), torch.tensor(begin, dtype=torch.int32).cuda(), table.cuda(), pg, n)
     torch.cuda.synchronize()
     assert torch.equal(K.cpu().view(torch.int16), want[0].view(torch.int16)) and torch.equal(V.cpu().view(torch.int16), want[1].view(torch.int16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hkv", [1, 2])
+def test_append_rows_of_any_dense_view(Hkv):
+    """One token or one head by transposition: that dimension's stride says nothing."""
+    P, t = 16, torch.float16
+    pg = ds.pages(3, P, Hkv, D, 1, 3)
+    table, new_start = torch.tensor([[2, 0, 1]], dtype=torch.int32).cuda(), lambda n: torch.tensor([0, n], dtype=torch.int32).cuda()
+    for n in (1, 5):
+        for form in ("dense", "heads_first", "slice"):
+            if form == "slice":
+                k, v = (values((n, Hkv + 3, D), t, i).cuda()[:, 1:1 + Hkv] for i in (1, 2))
+            elif form == "dense":
+                k, v = (values((n, Hkv, D), t, i).cuda() for i in (1, 2))
+            elif n == 1 or Hkv == 1:
+                k, v = (values((Hkv, n, D), t, i).cuda().transpose(0, 1) for i in (1, 2))
+            else:
+                continue
+            K = torch.zeros((3, Hkv, P, D), dtype=t, device="cuda")
+            V = torch.zeros_like(K)
+            ds.ds_append_paged(k, v, K, V, new_start(n), None, torch.tensor([18], dtype=torch.int32).cuda(), table, pg, 1)
+            want = torch.zeros_like(K), torch.zeros_like(K)
+            for w, x in zip(want, (k, v)):
+                w[0, :, 2:2 + n] = x.transpose(0, 1)
+            assert torch.equal(K, want[0]) and torch.equal(V, want[1]), (n, form)
+
+
+def test_append_rows_that_cannot_be():
+    pg = ds.pages(**PG)
+    x, i = torch.zeros(4, 2, D), torch.zeros(4, dtype=torch.int32)
+    for k, v in ((x[:, :1], x[:, :1]), (x[..., :64], x[..., :64]), (x[:3], x), (x, x[::2].repeat(2, 1, 1)[:3]), (x.transpose(0, 1).contiguous().transpose(0, 1), x),
+                 (torch.zeros(4, D, 2).transpose(1, 2), x), (torch.zeros(4, 3, D)[:, :2], x)):
+        with pytest.raises(ValueError, match="new rows|the same"):
+            ds.ds_append_paged(k, v, x, x, i, i, i, i, pg, 1)
