@@ -347,7 +347,9 @@ ds_status_t ds_attend_rows(const void *q, const void *KV_rows, float *out,
  * Keys that a row does not see have no part in it, whatever they and their values hold, infinities and NaN
  * too.  Rows that see such a value, or stand beside one in a tile, and rows whose sums overflow (bf16) are formed a second time,
  * after which sums of finite values are finite; a call all of whose rows are takes some five times as long.
- * max_kv: keys of the longest sequence (a guide to the split, which the results do not rest on).
+ * max_kv: keys of the longest sequence (a guide to the split, which the results do not rest on, but bits of a sum may; they may
+ * also rest on the rows beside a row, whose maxima are raised together).
+ * q and out may be NULL where total_q is 0, K and V where kv_elems is 0 (packed); k_new and v_new of ds_append_paged where total_new is.
  */
 typedef enum { DS_F16 = 0, DS_BF16 = 1 } ds_dtype_t; /* IEEE binary16; bfloat16 */
 

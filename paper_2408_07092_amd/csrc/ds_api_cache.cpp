@@ -90,7 +90,9 @@ ds_status_t ds_prompt_attention(const void *q, const void *K, const void *V, voi
                                 const int32_t *kv_start, const int32_t *kv_len, void *workspace,
                                 size_t workspace_bytes, const ds_prompt_t *prm, void *stream)
 {
-    if (!q || !K || !V || !out || !q_start || !kv_start || !kv_len || !workspace || !prm) return DS_ERR_NULL;
+    if (!q_start || !kv_start || !kv_len || !workspace || !prm) return DS_ERR_NULL;
+    // (arrays without an element may have no address)
+    if (((!q || !out) && prm->total_q != 0) || ((!K || !V) && prm->kv_elems != 0)) return DS_ERR_NULL;
     ds_prompt_t m;
     PromptPlan p;
     if (!prompt_ok(prm, &m)) return DS_ERR_SHAPE;
@@ -111,8 +113,8 @@ ds_status_t ds_prompt_attention_paged(const void *q, const void *K_pages, const 
                                       const int32_t *table, void *workspace, size_t workspace_bytes,
                                       const ds_prompt_t *prm, const ds_pages_t *pages, void *stream)
 {
-    if (!q || !K_pages || !V_pages || !out || !q_start || !lens || !table || !workspace || !prm || !pages)
-        return DS_ERR_NULL;
+    if (!K_pages || !V_pages || !q_start || !lens || !table || !workspace || !prm || !pages) return DS_ERR_NULL;
+    if ((!q || !out) && prm->total_q != 0) return DS_ERR_NULL;
     ds_prompt_t m;
     PromptPlan p;
     if (!prompt_ok(prm, &m) || !pages_ok(pages)) return DS_ERR_SHAPE;
@@ -190,7 +192,7 @@ ds_status_t ds_append_paged(const void *k_new, const void *v_new, void *K_pages,
                             const int32_t *table, const ds_pages_t *pages, int32_t n_seqs, int32_t total_new,
                             int64_t new_stride, void *stream)
 {
-    if (!k_new || !v_new || !K_pages || !V_pages || !new_start || !start || !table || !pages) return DS_ERR_NULL;
+    if (!K_pages || !V_pages || !new_start || !start || !table || !pages || ((!k_new || !v_new) && total_new != 0)) return DS_ERR_NULL;
     if (!pages_ok(pages) || n_seqs < 1 || total_new < 0 || (!rows && n_seqs > pages->n_rows)) return DS_ERR_SHAPE;
     const int64_t row = (int64_t)pages->Hkv * kD;
     if (new_stride == 0) new_stride = row;

@@ -70,6 +70,15 @@ def test_paged_refusals():
     assert call_paged(ok, ds.pages(**pg), n=ds.ds_prompt_workspace_bytes(ok) - 1) == ds.DS_ERR_WORKSPACE
 
 
+def test_arrays_without_an_element_need_no_address():
+    none = ds.prompt(**{**GOOD, "total_q": 0})
+    assert call(none, q=None, out=None) == ds.DS_OK and call(ds.prompt(**{**GOOD, "total_q": 0, "kv_elems": 0}), q=None, K=None, V=None, out=None) == ds.DS_OK
+    assert call(none, K=None) == ds.DS_ERR_NULL and call(none, q=None, kl=None) == ds.DS_ERR_NULL
+    assert call(ds.prompt(**{**GOOD, "total_q": -1}), q=None) == ds.DS_ERR_NULL
+    pg = ds.pages(n_pages=10, page_tokens=16, Hkv=2, d=D, n_rows=3, max_pages=4)
+    assert call_paged(none, pg, q=None, out=None) == ds.DS_OK and call_paged(none, pg, K=None) == ds.DS_ERR_NULL
+
+
 # ------------------------------------------------------------------ definition
 def defined(q, k, v, before):
     """(y, A, e): q [m, Hq, d], k and v [t, Hkv, d], row i sees the keys up to i + before."""
@@ -631,6 +640,22 @@ def test_which_rows_a_missing_page_makes_nan(heads, guide):
         for i in (0, 2):
             o = slice(int(qs[i]), int(qs[i + 1]))
             near(out[o], q[o], kv[i][0], kv[i][1], before[i], t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_no_rows_and_no_keys(dtype):
+    """Empty tensors, which have no address: no new tokens is nothing to do, no keys is rows of zeros."""
+    t, code = TYPES[dtype]
+    for rows, guide in ((0, 0), (40, 0), (3, 30000)):
+        q, K, out = values((rows, 4, D), t, 1).cuda(), torch.empty((0, 2, D), dtype=t, device="cuda"), torch.full((rows, 4, D), CANARY, dtype=t, device="cuda")
+        prm = ds.prompt(2, 4, 2, D, rows, guide, code)
+        ds.ds_prompt_attention(q, K, K, out, ints_([0, rows // 3, rows]), ints_([0, 0]), ints_([0, 0]), ds.ds_prompt_workspace_alloc(prm), prm)
+        assert (out == 0).all()
+    pg = ds.pages(1, 16, 2, D, 1, 1, code)
+    pool = torch.full((1, 2, 16, D), 3.0, dtype=t, device="cuda")
+    ds.ds_append_paged(K, K, pool, pool, ints_([0, 0]), None, ints_([0]), ints_([[0]]), pg, 1)
+    assert (pool == 3.0).all()
 
 
 def ints_(x):
