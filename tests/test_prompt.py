@@ -658,5 +658,58 @@ def test_no_rows_and_no_keys(dtype):
     assert (pool == 3.0).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(20, 1), (40, 2), (64, 1), (200, 1)], ids=str)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_groups_of_more_than_16_heads(dtype, heads):
+    """... up to more heads in a group than a row tile has rows."""
+    t, code, (Hq, Hkv), new, before = *TYPES[dtype], heads, [1, 70, 33], [5, 0, 100]
+    keys = [a + b for a, b in zip(new, before)]
+    T, qs, ks = sum(new), starts(new), starts(keys)
+    q, K, V = values((T, Hq, D), t, 1).cuda(), values((sum(keys), Hkv, D), t, 2, True).cuda(), values((sum(keys), Hkv, D), t, 3).cuda()
+    out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+    prm = ds.prompt(3, Hq, Hkv, D, T, max(keys), code, kv_elems=K.numel())
+    ds.ds_prompt_attention(q, K, V, out, qs.cuda(), ks[:-1].contiguous().cuda(), ints_(keys), ds.ds_prompt_workspace_alloc(prm), prm)
+    for i, (m, n, b) in enumerate(zip(new, keys, before)):
+        o, r = int(qs[i]), int(ks[i])
+        near(out[o:o + m], q[o:o + m], K[r:r + n], V[r:r + n], b, t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_long_prompts(dtype):
+    """Many tiles ahead of the causal edge, with heads alone and in pairs."""
+    t, code = TYPES[dtype]
+    for Hq, Hkv, new, before in ((2, 2, [5003], [0]), (2, 1, [3000, 1200], [1100, 4000])):
+        keys = [a + b for a, b in zip(new, before)]
+        T, qs, ks = sum(new), starts(new), starts(keys)
+        q, K, V = values((T, Hq, D), t, 1).cuda(), values((sum(keys), Hkv, D), t, 2, True).cuda(), values((sum(keys), Hkv, D), t, 3).cuda()
+        out = torch.full((T, Hq, D), CANARY, dtype=t, device="cuda")
+        prm = ds.prompt(len(new), Hq, Hkv, D, T, max(keys), code, kv_elems=K.numel())
+        ds.ds_prompt_attention(q, K, V, out, qs.cuda(), ks[:-1].contiguous().cuda(), ints_(keys), ds.ds_prompt_workspace_alloc(prm), prm)
+        for i, (m, n, b) in enumerate(zip(new, keys, before)):
+            o, r = int(qs[i]), int(ks[i])
+            near(out[o:o + m], q[o:o + m], K[r:r + n], V[r:r + n], b, t)
+
+
+@pytest.mark.gpu
+def test_caches_beyond_32_bit_offsets():
+    """Contiguous caches of more than 2^32 elements: the last head of the last entry, as of the first, split and whole."""
+    t, Hq, Hkv, L_max, n = torch.float16, 16, 8, 2_200_000, 400
+    K, V = (torch.empty((2, Hkv, L_max, D), dtype=t, device="cuda") for _ in range(2))
+    assert K.numel() > 1 << 32
+    rows = values((2, 2, Hkv, n, D), t, 4).cuda()
+    for b in range(2):
+        K[b, :, :n], V[b, :, :n] = rows[b, 0], rows[b, 1]
+    q, out = values((200, Hq, D), t, 1).cuda(), torch.empty((200, Hq, D), dtype=t, device="cuda")
+    for guide in (0, 5000):
+        prm = ds.prompt(2, Hq, Hkv, D, 200, guide, ds.DS_F16, kv_stride=D, kv_head_stride=L_max * D, kv_elems=K.numel())
+        ws = ds.ds_prompt_workspace_alloc(prm)
+        assert (ws.numel() > 256) == (guide > 0)
+        ds.ds_prompt_attention(q, K, V, out.fill_(CANARY), ints_([0, 100, 200]), ints_([0, Hkv * L_max]), ints_([n, n]), ws, prm)
+        for b in range(2):
+            near(out[100 * b:100 * b + 100], q[100 * b:100 * b + 100], rows[b, 0].transpose(0, 1), rows[b, 1].transpose(0, 1), n - 100, t)
+
+
 def ints_(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
