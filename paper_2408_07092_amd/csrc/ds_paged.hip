@@ -495,7 +495,7 @@ void make_paged_plan(const ds_pages_t &g, int n, int Hq, int max_len, PagedPlan 
     p->G = Hq / g.Hkv;
     p->passes = (p->G + 15) / 16;
     p->GH = p->G <= 4 ? 4 : p->G <= 8 ? 8 : 16;
-    const int64_t units = (int64_t)n * g.Hkv * p->passes, pieces = units * std::max(1, (max_len + kPiece - 1) / kPiece);
+    const int64_t units = (int64_t)n * g.Hkv * p->passes, pieces = units * std::max<int64_t>(1, ((int64_t)max_len + kPiece - 1) / kPiece);
     // One workgroup to a compute unit reads fastest.  Where units are many and short it waits for one's lengths, page and rows after
     // the other's, and a second one is worth its bandwidth: 65 sequences of up to 24 tokens, 40 heads 25.5 us with one and 15.9 with two,
     // 32 of up to 200, 32 heads 26.8 and 25.1; on the other side 128 of up to 500, 8 groups of 8 50.2 and 52.5, one of 900, 32

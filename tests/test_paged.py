@@ -270,6 +270,30 @@ def test_decode_values_that_are_not_finite(dtype, guide):
 
 
 @pytest.mark.gpu
+def test_decode_with_the_largest_guide():
+    """max_len of 2^31 - 1 plans for long sequences, not for none: all compute units share one of 60000 tokens."""
+    t, code, P, Hq, Hkv, n = torch.float16, ds.DS_F16, 64, 4, 1, 60000
+    Kp, Vp, table, kv = paged([n], Hkv, P, t, 38)
+    table, lens, q = table[1:2].contiguous(), torch.tensor([n], dtype=torch.int32).cuda(), values((1, Hq, D), t, 1).cuda()
+    pg = ds.pages(Kp.shape[0], P, Hkv, D, 1, table.shape[1], code)
+    took = []
+    for guide in (n, 2**31 - 1):
+        out, ws = torch.zeros((1, Hq, D), device="cuda"), ds.ds_paged_workspace_alloc(pg, 1, Hq, guide)
+        run = lambda: ds.ds_paged_decode(q, Kp, Vp, out, None, lens, table, ws, pg, 1, Hq, guide)  # noqa: E731
+        run()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(20):
+            run()
+        b.record()
+        torch.cuda.synchronize()
+        took.append(a.elapsed_time(b) * 50)
+        near(out[0], q[0], kv[0][0], kv[0][1], t)
+    print(f"{took[0]:.0f} and {took[1]:.0f} us")
+    assert took[1] < 4 * took[0]
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("heads", [(2, 2), (24, 2)], ids=str)
 def test_decode_workspace_serves_other_batches(heads):
     """One workspace, cleared once, for more and fewer sequences in turn: what one call leaves of its parts is not where
