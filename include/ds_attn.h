@@ -333,8 +333,8 @@ ds_status_t ds_attend_rows(const void *q, const void *KV_rows, float *out,
  *     kv_elems: elements from K (and from V) that may be read.
  *   ds_prompt_attention_paged: the keys are the first lens[row] tokens of page table row rows[s] (rows NULL:
  *     row s); see ds_pages_t.  prm->kv_stride, kv_head_stride and kv_elems are not used.
- * Accumulation and softmax statistics are binary32; the weights are rounded once to the type of V, outputs
- * once to the type of q.
+ * Accumulation and softmax statistics are binary32 (a score beyond its range is infinite); the weights are rounded once to the
+ * type of V, outputs once to the type of q.
  * Argument checks: strides are multiples of 8 elements (0: the dense value, Hq * d for q and out, Hkv * d
  * and d for kv_stride and kv_head_stride); q, K, V and out 16-byte aligned, pools of pages 256-byte.
  * n_seqs < 1, total_q < 0, max_kv < 0, bad heads, d != 128, a stride below the row it steps over or

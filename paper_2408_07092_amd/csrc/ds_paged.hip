@@ -11,7 +11,7 @@
 // which tokens follows from the lengths and the launch alone, so results do not depend on who is last.
 //
 // One workgroup to a compute unit, each wavefront with two tiles of 16 tokens on their way (64 KiB a compute unit), streams best: 16
-// sequences of 32K tokens (2.1 GB) take 319 us, 6.7 TB/s, one of 250K (512 MB) 85.  (As first measured: 322, and with one tile on
+// sequences of 32K tokens (2.1 GB) take 319 us, 6.7 TB/s, one of 250K (512 MB) 86.  (As first measured: 322, and with one tile on
 // its way and one, two or four workgroups 405, 318 and 347, with two tiles and two workgroups 332; 89, and 118 to 182 with one
 // tile and two to four workgroups, whose parts cost more to join.  Three and four tiles: no difference.)  A unit's beginning and end (its query, the
 // wavefronts' states, the part) cost a workgroup about what three pieces do, and count as kLead pieces: 48 sequences of 3 to 20000

@@ -5,10 +5,10 @@
 //
 // over the keys j <= i + nk - nq, in one pass over the keys with a running maximum m and a
 // running sum.  Bound by the matrix units: 4 d flops a pair against a few bytes for each row.  8K tokens of 32 heads take
-// 528 us (1.04 PFLOP/s), two of 8K in groups of 4 986 us; a library product of 16384 x 16384 x 16384 reaches 1.3 to 1.37.  What
-// holds it there is power: the same launch on zeros takes 352 us, and on random data the clock is at 1.6 to 1.7 GHz, with
-// the matrix units busy in 58 % of the cycles.  Short prompts are bound by a workgroup's steps one after the other, 1.2 us each
-// with the compute unit to itself (97 tokens 6.5 us, 500 in groups of 4 14.8, 1500 of 32 heads 39).
+// 528 us (1.04 PFLOP/s), two of 8K in groups of 4 982 us; a library product of 16384 x 16384 x 16384 reaches 1.3 to 1.37.  What
+// holds it there is power: the same launch on zeros takes 365 us, and on random data the clock is at 1.6 to 1.7 GHz, with
+// the matrix units busy in 60 % of the cycles.  Short prompts are bound by a workgroup's steps one after the other, 1.2 us each
+// with the compute unit to itself (97 tokens 6.6 us, 500 in groups of 4 14.8, 1500 of 32 heads 39).
 //
 // The G query heads of a KV head are rows of one matrix: row token * G + g.  A workgroup takes 128 of
 // these rows, a wavefront 32, and walks the keys in tiles of 64 that all of its wavefronts share from LDS.  Two
